@@ -364,6 +364,51 @@ int ovggt_k_gemm_bf16(const void* A, const void* B, int32_t M, int32_t N, int32_
 int ovggt_k_linear_bf16(const void* A, const void* B, int32_t M, int32_t N, int32_t K, void* const* outs, int32_t n_outs,
                         int32_t gelu, const void* residual, void* sum, int32_t* device_status, void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * A block in 8 bits: its rows and weights as int8 with fp32 scales, its keys and values in an 8-bit cache.  Not a step of
+ * the paper's path either; it stands beside the bf16 product and the attention above for models served in 8 bits.
+ * ---------------------------------------------------------------------------------------------- */
+
+/* What the rows become before they are quantised: nothing, x / sqrt(mean(x^2) + eps), or (x - mean) / sqrt(variance + eps). */
+enum { OVGGT_NORM_NONE = 0, OVGGT_NORM_RMS = 1, OVGGT_NORM_LAYER = 2 };
+
+/* h = x + residual (rounded to dtype), or x; y = norm(h) * weight + bias; scale[row] = max |y| / 127, q = round(y / scale), ties
+ * to even.  x, residual, sum [rows, C], weight, bias [C] in dtype; q [rows, C] int8; scale [rows] fp32.  residual, weight, bias and sum may
+ * be NULL (weight and bias are NULL for OVGGT_NORM_NONE); sum takes h and needs a residual; it may be x or residual.  Statistics are
+ * fp32.  A row whose y is not finite gets a scale that is not a number and zeros in q; one whose |y| stays below 2^-119 a
+ * scale of 0 and zeros.  C a multiple of 16, up to 16384 (OVGGT_ERR_UNSUPPORTED). */
+int ovggt_k_norm_q8(const void* x, const void* residual, const void* weight, const void* bias, int32_t rows, int32_t C,
+                    int32_t dtype, int32_t kind, float eps, void* sum, int8_t* q, float* scale, void* stream);
+
+/* The product of ovggt_k_linear_bf16 on int8 rows: t = bf16(a_scale[m] w_scale[n] sum_k A[m, k] W[n, k]), A [M, K], W [N, K] (a row of
+ * weights for each channel), a_scale [M], w_scale [N] fp32; the sums are int32 and exact.  gelu, outs, n_outs, residual, sum and
+ * device_status as there (sum may be residual here).  K a multiple of 16, up to 131056; N a multiple of 8 (OVGGT_ERR_UNSUPPORTED). */
+int ovggt_k_linear_q8(const int8_t* A, const float* a_scale, const int8_t* W, const float* w_scale, int32_t M, int32_t N, int32_t K,
+                      void* const* outs, int32_t n_outs, int32_t gelu, const void* residual, void* sum, int32_t* device_status,
+                      void* stream);
+
+/* An 8-bit cache is four device arrays: kq, vq [n_seqs, capacity, n_heads * 64] int8 and kx, vx [n_seqs, n_heads, capacity] uint8.  The 64
+ * columns of a row and head are a block: with e = floor(log2(max |x|)), at least -120, it holds q = round(x 2^(6 - e)), at most 127 in
+ * size, and the byte e + 127; its values q 2^(e - 6) are exact in bf16, so reading rounds nothing and writing what was
+ * read back gives the same bytes.  A block that is not finite has the byte 255 and reads as NaN.  capacity a multiple of 16, head_dim 64.
+ *
+ * ovggt_k_store_q8: rows k, v [n_seqs, M, n_heads * 64] in dtype to rows start[s] .. start[s] + M - 1 of sequence s (start: device
+ * [n_seqs], NULL = 0).  A sequence whose start is negative is left alone, and so is what would lie beyond the capacity.
+ * ovggt_k_load_q8: rows first .. first + n - 1 of every sequence to k, v [n_seqs, n, n_heads * 64] in dtype. */
+int ovggt_k_store_q8(const void* k, const void* v, int32_t n_seqs, int32_t M, int32_t n_heads, int32_t dtype, const int32_t* start,
+                     int32_t capacity, int8_t* kq, uint8_t* kx, int8_t* vq, uint8_t* vx, void* stream);
+int ovggt_k_load_q8(const int8_t* kq, const uint8_t* kx, const int8_t* vq, const uint8_t* vx, int32_t n_seqs, int32_t n_heads,
+                    int32_t capacity, int32_t first, int32_t n, int32_t dtype, void* k, void* v, void* stream);
+
+/* out [n_seqs, M, n_heads * 64] = softmax(Q K^T / sqrt(64)) V over the rows of an 8-bit cache, bf16 queries and output: row j of sequence s
+ * takes part if j < lens[s] (device [n_seqs], NULL = capacity; taken as 0 below 0 and as capacity above it) and live[s, j] != 0 (device
+ * [n_seqs, capacity] uint8, NULL = all).  Where no row does, out is 0.  Query head h reads key head h / (n_heads / n_kv_heads); n_heads
+ * a multiple of n_kv_heads.  Rows that do not take part are not looked at: they may hold anything.  device_status: device int, as for
+ * ovggt_k_attention.  No scratch memory. */
+int ovggt_k_attention_q8(const void* q, const int8_t* kq, const uint8_t* kx, const int8_t* vq, const uint8_t* vx, int32_t n_seqs,
+                         int32_t M, int32_t n_heads, int32_t n_kv_heads, int32_t capacity, const int32_t* lens, const uint8_t* live,
+                         void* out, int32_t* device_status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

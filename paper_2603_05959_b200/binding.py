@@ -22,6 +22,7 @@ DTYPE_F32, DTYPE_BF16 = 0, 1
 SCORE_HYBRID, SCORE_RESIDUAL_STORED, SCORE_RANDOM, SCORE_QK, SCORE_ATTN = 0, 1, 2, 3, 4
 FLAG_EVICTABLE, FLAG_INIT, FLAG_HIST = 0, 1, 2
 COMPACT_FILL_HOLES, COMPACT_STABLE_GATHER = 0, 1
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 PROF_CLASSES = ["append", "attention", "row_norms", "diversity", "select", "compact"]
 
 EXPORTED = [
@@ -33,7 +34,8 @@ EXPORTED = [
     "ovggt_strerror", "ovggt_last_cuda_error", "ovggt_k_row_norms", "ovggt_k_diversity_scratch_bytes",
     "ovggt_k_diversity", "ovggt_k_diversity_static", "ovggt_k_select", "ovggt_k_compact", "ovggt_k_attention_scratch_bytes",
     "ovggt_k_attention", "ovggt_k_key_norm_bound", "ovggt_k_attention_bounded", "ovggt_k_gemm_bf16",
-    "ovggt_k_linear_bf16",
+    "ovggt_k_linear_bf16", "ovggt_k_norm_q8", "ovggt_k_linear_q8", "ovggt_k_store_q8", "ovggt_k_load_q8",
+    "ovggt_k_attention_q8",
 ]
 
 
@@ -127,6 +129,11 @@ def lib():
         L.ovggt_k_key_norm_bound.argtypes = [vp, i32, i32, vp, vp]
         L.ovggt_k_gemm_bf16.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp]
         L.ovggt_k_linear_bf16.argtypes = [vp, vp, i32, i32, i32, C.POINTER(vp), i32, i32, vp, vp, vp, vp]
+        L.ovggt_k_norm_q8.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, C.c_float, vp, vp, vp, vp]
+        L.ovggt_k_linear_q8.argtypes = [vp, vp, vp, vp, i32, i32, i32, C.POINTER(vp), i32, i32, vp, vp, vp, vp]
+        L.ovggt_k_store_q8.argtypes = [vp, vp, i32, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp]
+        L.ovggt_k_load_q8.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp]
+        L.ovggt_k_attention_q8.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp]
         L.ovggt_k_attention_bounded.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp]
         assert _FRAME_IO.size == C.sizeof(OvggtFrameIO)
         for name in ("ovggt_layer_attend", "ovggt_layer_compress", "ovggt_layer_step", "ovggt_layer_step_host"):
@@ -527,4 +534,108 @@ def k_attention(q, k, v, n_heads: int, out=None, scratch=None, status=None, stre
     if own_status:
         code = int(status[0].item())
         _check(code, "ovggt_k_attention (device status)")
+    return out
+
+
+# ------------------------------------------------------------------ a block in 8 bits
+
+def _dtype_of(t: torch.Tensor) -> int:
+    assert t.dtype in (torch.float32, torch.bfloat16)
+    return DTYPE_F32 if t.dtype == torch.float32 else DTYPE_BF16
+
+
+def _here(*tensors: Optional[torch.Tensor]) -> None:
+    """The kernels run on the current device: so do their tensors."""
+    device = torch._C._cuda_getDevice()
+    assert all(t is None or t.get_device() == device for t in tensors), "tensors of another device than the current one"
+
+
+def k_norm_q8(x: torch.Tensor, weight=None, bias=None, residual=None, kind=NORM_RMS, eps=1e-6, sum_out=None, q=None, scale=None,
+              stream=None):
+    """(q int8 like x, scale fp32 [...]): the rows of x [..., C] (+ residual, the sum to sum_out) normalised and quantised."""
+    dtype, width = _dtype_of(x), x.shape[-1]
+    q = torch.empty(x.shape, dtype=torch.int8, device=x.device) if q is None else q
+    scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if scale is None else scale
+    assert all(t.dtype == x.dtype and t.shape == x.shape for t in (residual, sum_out) if t is not None)
+    assert all(t.dtype == x.dtype and t.shape == (width,) for t in (weight, bias) if t is not None)
+    assert q.dtype == torch.int8 and q.shape == x.shape and scale.dtype == torch.float32 and scale.shape == x.shape[:-1]
+    _here(x, weight, bias, residual, sum_out, q, scale)
+    _check(lib().ovggt_k_norm_q8(_dptr(x), _dptr(residual), _dptr(weight), _dptr(bias), x.numel() // width if width else 0, width, dtype, kind, eps,
+                                 _dptr(sum_out), _dptr(q), _dptr(scale), _stream_ptr(stream)), "ovggt_k_norm_q8")
+    return q, scale
+
+
+def k_linear_q8(a, a_scale, w, w_scale, outs=(), gelu=False, residual=None, sum_out=None, status=None, stream=None) -> None:
+    """t = (a a_scale) [M, K] @ (w w_scale) [N, K] ^T (then GELU), int8 operands; its column blocks to outs; sum_out = residual + t.
+    Nothing is allocated."""
+    (M, K), N = a.shape, w.shape[0]
+    assert w.shape[1] == K and a.dtype == torch.int8 and w.dtype == torch.int8
+    assert a_scale.shape == (M,) and w_scale.shape == (N,) and a_scale.dtype == torch.float32 and w_scale.dtype == torch.float32
+    assert all(t.dtype == torch.bfloat16 for t in (residual, sum_out, *outs) if t is not None)
+    assert all(o.numel() * len(outs) == M * N for o in outs) and len(outs) <= 3
+    assert all(t.numel() == M * N for t in (residual, sum_out) if t is not None) and status.numel() * status.element_size() >= 4
+    _here(a, a_scale, w, w_scale, residual, sum_out, status, *outs)
+    _check(lib().ovggt_k_linear_q8(_dptr(a), _dptr(a_scale), _dptr(w), _dptr(w_scale), M, N, K, (C.c_void_p * 3)(*[_dptr(o) for o in outs]),
+                                   len(outs), int(gelu), _dptr(residual), _dptr(sum_out), _dptr(status), _stream_ptr(stream)),
+           "ovggt_k_linear_q8")
+
+
+def new_cache_q8(n_seqs: int, capacity: int, n_heads: int, device=None):
+    """(kq, kx, vq, vx): an empty 8-bit cache for the calls below, a capacity of whole sixteens."""
+    device = device or torch.device("cuda", torch.cuda.current_device())
+    rows = (capacity + 15) // 16 * 16
+    new = lambda *shape, dtype: torch.zeros(shape, dtype=dtype, device=device)
+    return (new(n_seqs, rows, n_heads * 64, dtype=torch.int8), new(n_seqs, n_heads, rows, dtype=torch.uint8),
+            new(n_seqs, rows, n_heads * 64, dtype=torch.int8), new(n_seqs, n_heads, rows, dtype=torch.uint8))
+
+
+def _cache_q8(cache):
+    """(n_seqs, capacity, n_heads) of an 8-bit cache's four tensors."""
+    kq, kx, vq, vx = cache
+    assert kq.dtype == vq.dtype == torch.int8 and kx.dtype == vx.dtype == torch.uint8
+    n_seqs, capacity, width = kq.shape
+    assert width % 64 == 0 and vq.shape == kq.shape and kx.shape == vx.shape == (n_seqs, width // 64, capacity)
+    return n_seqs, capacity, width // 64
+
+
+def k_store_q8(cache, k: torch.Tensor, v: torch.Tensor, start=None, stream=None) -> None:
+    """Rows k, v [n_seqs, M, C] into the cache (kq, kx, vq, vx), from row start[s] (int32 [n_seqs]; None: 0) of each sequence on."""
+    n_seqs, capacity, H = _cache_q8(cache)
+    assert k.shape == v.shape and k.dtype == v.dtype and k.dim() == 3 and (k.shape[0], k.shape[2]) == (n_seqs, H * 64)
+    assert start is None or (start.dtype == torch.int32 and start.shape == (n_seqs,))
+    _here(*cache, k, v, start)
+    kq, kx, vq, vx = cache
+    _check(lib().ovggt_k_store_q8(_dptr(k), _dptr(v), n_seqs, k.shape[1], H, _dtype_of(k), _dptr(start), capacity, _dptr(kq), _dptr(kx),
+                                  _dptr(vq), _dptr(vx), _stream_ptr(stream)), "ovggt_k_store_q8")
+
+
+def k_load_q8(cache, n: int, first: int = 0, dtype=torch.bfloat16, stream=None):
+    """(k, v) [n_seqs, n, C]: rows first .. first + n - 1 of every sequence, exact."""
+    n_seqs, capacity, H = _cache_q8(cache)
+    k, v = (torch.empty((n_seqs, max(n, 0), H * 64), dtype=dtype, device=cache[0].device) for _ in range(2))
+    _here(*cache)
+    kq, kx, vq, vx = cache
+    _check(lib().ovggt_k_load_q8(_dptr(kq), _dptr(kx), _dptr(vq), _dptr(vx), n_seqs, H, capacity, int(first), int(n), _dtype_of(k), _dptr(k),
+                                 _dptr(v), _stream_ptr(stream)), "ovggt_k_load_q8")
+    return k, v
+
+
+def k_attention_q8(q: torch.Tensor, cache, lens=None, live=None, out=None, status=None, stream=None) -> torch.Tensor:
+    """softmax(q k / 8) v of queries q [n_seqs, M, heads * 64] (bf16) over the cache's live rows (uint8 [n_seqs, capacity]; None: all)
+    within lens (int32 [n_seqs]; None: the capacity); 0 where there is none."""
+    n_seqs, capacity, H = _cache_q8(cache)
+    assert q.dtype == torch.bfloat16 and q.dim() == 3 and q.shape[0] == n_seqs and q.shape[2] % 64 == 0
+    assert lens is None or (lens.dtype == torch.int32 and lens.shape == (n_seqs,))
+    assert live is None or (live.dtype == torch.uint8 and live.shape == (n_seqs, capacity))
+    out = torch.empty_like(q) if out is None else out
+    assert out.dtype == q.dtype and out.shape == q.shape
+    own = status is None
+    if own:
+        status = torch.zeros(16, dtype=torch.int32, device=q.device)
+    _here(q, *cache, lens, live, out, status)
+    kq, kx, vq, vx = cache
+    _check(lib().ovggt_k_attention_q8(_dptr(q), _dptr(kq), _dptr(kx), _dptr(vq), _dptr(vx), n_seqs, q.shape[1], q.shape[2] // 64, H, capacity,
+                                      _dptr(lens), _dptr(live), _dptr(out), _dptr(status), _stream_ptr(stream)), "ovggt_k_attention_q8")
+    if own:
+        _check(int(status[0].item()), "ovggt_k_attention_q8 (device status)")
     return out

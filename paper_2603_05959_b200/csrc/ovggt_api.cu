@@ -16,11 +16,14 @@
 
 #include "../../include/ovggt.h"
 #include "attn_f32.cuh"
+#include "attn_q8.cuh"
 #include "attn_tcgen05.cuh"
 #include "common.cuh"
 #include "compact_kernels.cuh"
 #include "front_kernel.cuh"
+#include "gemm_q8.cuh"
 #include "gemm_tcgen05.cuh"
+#include "q8_rows.cuh"
 #include "score_kernels.cuh"
 #include "select_kernel.cuh"
 #include "token_kernel.cuh"
@@ -51,7 +54,8 @@ inline int cuda_fail(cudaError_t e) {
   } while (0)
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+inline bool aligned16(const void* p) { return aligned(p, 16); }
 
 constexpr int kMaxColsumParts = 592;       // 4 CTAs per SM on 148 SMs
 constexpr size_t kSmemLimit = 227 * 1024;
@@ -1588,6 +1592,121 @@ extern "C" int ovggt_k_gemm_bf16(const void* A, const void* Bm, int32_t M, int32
                                  int32_t* device_status, void* stream) {
   if (!C) return OVGGT_ERR_INVALID_ARG;
   return ovggt_k_linear_bf16(A, Bm, M, N, K, &C, 1, 0, nullptr, nullptr, device_status, stream);
+}
+
+// ------------------------------------------------------------------ a block in 8 bits
+
+extern "C" int ovggt_k_norm_q8(const void* x, const void* residual, const void* weight, const void* bias, int32_t rows, int32_t C,
+                               int32_t dtype, int32_t kind, float eps, void* sum, int8_t* q, float* scale, void* stream) {
+  if (rows == 0) return OVGGT_OK;
+  if (!x || !q || !scale || rows < 0 || C < 1 || (dtype != kF32 && dtype != kBF16) || kind < OVGGT_NORM_NONE || kind > OVGGT_NORM_LAYER ||
+      (sum && !residual) || (kind == OVGGT_NORM_NONE && (weight || bias)) || !(eps >= 0.0f))
+    return OVGGT_ERR_INVALID_ARG;
+  if (C % 16 != 0 || C > kNormMaxC) return OVGGT_ERR_UNSUPPORTED;
+  if (!aligned16(x) || !aligned16(residual) || !aligned16(weight) || !aligned16(bias) || !aligned16(sum) || !aligned16(q) || !aligned(scale, 4))
+    return OVGGT_ERR_MISALIGNED;
+  NormQ8Args P = {};
+  P.x = static_cast<const uint4*>(x);
+  P.residual = static_cast<const uint4*>(residual);
+  P.weight = static_cast<const uint4*>(weight);
+  P.bias = static_cast<const uint4*>(bias);
+  P.sum = static_cast<uint4*>(sum);
+  P.q = reinterpret_cast<uint2*>(q);
+  P.scale = scale;
+  P.rows = rows; P.C = C; P.kind = kind; P.eps = eps;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  CK(dtype == kBF16 ? norm_q8_launch<kBF16>(P, st) : norm_q8_launch<kF32>(P, st));
+  LAUNCHED();
+  return OVGGT_OK;
+}
+
+extern "C" int ovggt_k_linear_q8(const int8_t* A, const float* a_scale, const int8_t* W, const float* w_scale, int32_t M, int32_t N,
+                                 int32_t K, void* const* outs, int32_t n_outs, int32_t gelu, const void* residual, void* sum,
+                                 int32_t* device_status, void* stream) {
+  if (M == 0) return OVGGT_OK;
+  if (!A || !a_scale || !W || !w_scale || !device_status || M < 0 || N < 1 || K < 1 || n_outs < 0 || n_outs > 3 ||
+      (n_outs > 0 && !outs) || (residual != nullptr) != (sum != nullptr) || (n_outs == 0 && !sum))
+    return OVGGT_ERR_INVALID_ARG;
+  if (K % 16 != 0 || K > kQ8MaxK || N % 8 != 0 || (n_outs > 1 && (N % n_outs != 0 || (N / n_outs) % 8 != 0))) return OVGGT_ERR_UNSUPPORTED;
+  if (!aligned16(A) || !aligned16(W) || !aligned(a_scale, 4) || !aligned16(w_scale) || !aligned16(residual) || !aligned16(sum))
+    return OVGGT_ERR_MISALIGNED;
+  GemmQ8Args P = {};
+  P.o.M = M; P.o.N = N; P.o.K = K;
+  for (int i = 0; i < n_outs; ++i) {
+    if (!outs[i]) return OVGGT_ERR_INVALID_ARG;
+    if (!aligned16(outs[i])) return OVGGT_ERR_MISALIGNED;
+    P.o.out[i] = static_cast<__nv_bfloat16*>(outs[i]);
+  }
+  P.o.part = n_outs > 1 ? N / n_outs : N;
+  P.o.gelu = gelu != 0;
+  P.o.residual = static_cast<const __nv_bfloat16*>(residual);
+  P.o.sum = static_cast<__nv_bfloat16*>(sum);
+  P.o.status = device_status;
+  P.a = A; P.w = W;
+  P.a_scale = a_scale; P.w_scale = w_scale;
+  const int rc = gemm_q8_launch(P, static_cast<cudaStream_t>(stream));
+  if (rc == OVGGT_OK) g_launches.fetch_add(1);
+  if (rc == OVGGT_ERR_CUDA) cuda_fail((cudaError_t)attn_tcgen05_last_error());
+  return rc;
+}
+
+extern "C" int ovggt_k_store_q8(const void* k, const void* v, int32_t n_seqs, int32_t M, int32_t n_heads, int32_t dtype,
+                                const int32_t* start, int32_t capacity, int8_t* kq, uint8_t* kx, int8_t* vq, uint8_t* vx, void* stream) {
+  if (n_seqs == 0 || M == 0) return OVGGT_OK;
+  if (!k || !v || !kq || !kx || !vq || !vx || n_seqs < 0 || M < 0 || n_heads < 1 || capacity < 1 || (dtype != kF32 && dtype != kBF16))
+    return OVGGT_ERR_INVALID_ARG;
+  if (capacity % 16 != 0) return OVGGT_ERR_UNSUPPORTED;
+  if (!aligned16(k) || !aligned16(v) || !aligned16(kq) || !aligned16(vq) || !aligned16(kx) || !aligned16(vx) || !aligned(start, 4))
+    return OVGGT_ERR_MISALIGNED;
+  const long long ctas = ((long long)n_seqs * M * n_heads * 8 + 255) / 256;
+  if (ctas > 0x7FFFFFFF) return OVGGT_ERR_UNSUPPORTED;
+  const StoreQ8Args P = {{static_cast<const uint4*>(k), static_cast<const uint4*>(v)}, {reinterpret_cast<uint2*>(kq), reinterpret_cast<uint2*>(vq)},
+                         {kx, vx}, start, n_seqs, M, n_heads, capacity};
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  CK(launch_dependent(dtype == kBF16 ? k_store_q8<kBF16> : k_store_q8<kF32>, dim3((unsigned)ctas, 2), 256, 1, 0, st, true, P));
+  LAUNCHED();
+  return OVGGT_OK;
+}
+
+extern "C" int ovggt_k_load_q8(const int8_t* kq, const uint8_t* kx, const int8_t* vq, const uint8_t* vx, int32_t n_seqs,
+                               int32_t n_heads, int32_t capacity, int32_t first, int32_t n, int32_t dtype, void* k, void* v, void* stream) {
+  if (n_seqs == 0 || n == 0) return OVGGT_OK;
+  if (!k || !v || !kq || !kx || !vq || !vx || n_seqs < 0 || n < 0 || n_heads < 1 || capacity < 1 || first < 0 ||
+      (long long)first + n > capacity || (dtype != kF32 && dtype != kBF16))
+    return OVGGT_ERR_INVALID_ARG;
+  if (capacity % 16 != 0) return OVGGT_ERR_UNSUPPORTED;
+  if (!aligned16(k) || !aligned16(v) || !aligned16(kq) || !aligned16(vq) || !aligned16(kx) || !aligned16(vx)) return OVGGT_ERR_MISALIGNED;
+  const long long ctas = ((long long)n_seqs * n * n_heads * 4 + 255) / 256;
+  if (ctas > 0x7FFFFFFF) return OVGGT_ERR_UNSUPPORTED;
+  const LoadQ8Args P = {{reinterpret_cast<const uint4*>(kq), reinterpret_cast<const uint4*>(vq)}, {kx, vx}, {k, v}, n_seqs, first, n, n_heads, capacity};
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  CK(launch_dependent(dtype == kBF16 ? k_load_q8<kBF16> : k_load_q8<kF32>, dim3((unsigned)ctas, 2), 256, 1, 0, st, true, P));
+  LAUNCHED();
+  return OVGGT_OK;
+}
+
+extern "C" int ovggt_k_attention_q8(const void* q, const int8_t* kq, const uint8_t* kx, const int8_t* vq, const uint8_t* vx, int32_t n_seqs,
+                                    int32_t M, int32_t n_heads, int32_t n_kv_heads, int32_t capacity, const int32_t* lens,
+                                    const uint8_t* live, void* out, int32_t* device_status, void* stream) {
+  if (n_seqs == 0 || M == 0) return OVGGT_OK;
+  if (!q || !kq || !kx || !vq || !vx || !out || !device_status || n_seqs < 0 || M < 0 || n_heads < 1 || n_kv_heads < 1 || capacity < 1 ||
+      n_heads % n_kv_heads != 0)
+    return OVGGT_ERR_INVALID_ARG;
+  if (capacity % 16 != 0 || (long long)M * n_heads > 0x7FFFFF00 || (long long)n_seqs * capacity > 0x7FFFFF00) return OVGGT_ERR_UNSUPPORTED;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(kq) || !aligned16(vq) || !aligned16(kx) || !aligned16(vx) || !aligned16(live) ||
+      !aligned(lens, 4) || !aligned(device_status, 4))
+    return OVGGT_ERR_MISALIGNED;
+  AttnQ8Args P = {};
+  P.q = static_cast<const __nv_bfloat16*>(q);
+  P.kq = kq; P.vq = vq; P.kx = kx; P.vx = vx;
+  P.lens = lens; P.live = live;
+  P.out = static_cast<__nv_bfloat16*>(out);
+  P.seqs = n_seqs; P.M = M; P.H = n_heads; P.HK = n_kv_heads; P.cap = capacity; P.group = n_heads / n_kv_heads;
+  P.status = device_status;
+  const int rc = attn_q8_launch(P, static_cast<cudaStream_t>(stream));
+  if (rc == OVGGT_OK) g_launches.fetch_add(1);
+  if (rc == OVGGT_ERR_CUDA) cuda_fail((cudaError_t)attn_tcgen05_last_error());
+  return rc;
 }
 
 // ------------------------------------------------------------------ allocation-free diversity

@@ -1,0 +1,278 @@
+// Rows in 8 bits: quantising rows behind a residual sum and a norm, and keys and values into and out of an 8-bit cache.
+#pragma once
+
+#include "attn_tcgen05.cuh"
+
+namespace ovggt {
+
+// Four floats, whole numbers of at most 127 in size after rounding, as int8 (round to nearest, ties to even): adding 1.5 * 2^23
+// leaves the whole number's two's complement in the low byte.
+__device__ __forceinline__ uint32_t pack_int8(float a, float b, float c, float d) {
+  const float magic = 12582912.0f;
+  const uint32_t x = __float_as_uint(a + magic), y = __float_as_uint(b + magic), z = __float_as_uint(c + magic), w = __float_as_uint(d + magic);
+  return __byte_perm(__byte_perm(x, y, 0x0040), __byte_perm(z, w, 0x0040), 0x5410);
+}
+
+// ---------------------------------------------------------------- rows to int8 with a scale each
+
+// One row is h = x + residual (rounded to the rows' type and stored), y = its norm, scale = max |y| / 127, q = round(y / scale).
+// The row stays in registers between its three reductions (mean, squares, maximum), so x and the residual are read once.
+struct NormQ8Args {
+  const uint4 *x, *residual, *weight, *bias;   // rows of C elements; residual, weight, bias may be nullptr
+  uint4* sum;                                  // h, or nullptr
+  uint2* q;
+  float* scale;
+  int rows, C, kind;
+  float eps;
+};
+
+template <int DT>
+__device__ __forceinline__ void load8(const uint4* p, size_t unit, float* f) {   // eight elements
+  if constexpr (DT == kBF16) {
+    unpack<DT>(p[unit], f);
+  } else {
+    unpack<DT>(p[2 * unit], f);
+    unpack<DT>(p[2 * unit + 1], f + 4);
+  }
+}
+
+// A value over the THREADS threads that hold a row: a warp's butterfly, then the warps' results in order.
+template <int THREADS, typename Op>
+__device__ __forceinline__ float row_reduce(float x, float* sh, Op op) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x = op(x, __shfl_xor_sync(0xFFFFFFFFu, x, o));
+  if constexpr (THREADS > 32) {
+    __syncthreads();                                     // (the scratch of the reduction before has been read)
+    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = x;
+    __syncthreads();
+    x = sh[0];
+#pragma unroll
+    for (int w = 1; w < THREADS / 32; ++w) x = op(x, sh[w]);
+  }
+  return x;
+}
+
+// UNITS groups of eight elements a thread, THREADS threads a row: a warp, or a CTA of 128 or 256.
+constexpr int kNormWarps = 4;                            // rows of a CTA where a warp takes a row
+template <int DT, int THREADS, int UNITS>
+__global__ void __launch_bounds__(THREADS == 32 ? kNormWarps * 32 : THREADS) k_norm_q8(const NormQ8Args P) {
+  __shared__ float sh[8];
+  pdl_trigger();
+  pdl_wait();
+  const int tid = THREADS == 32 ? threadIdx.x & 31 : threadIdx.x;
+  const long long row = THREADS == 32 ? (long long)blockIdx.x * kNormWarps + (threadIdx.x >> 5) : blockIdx.x;
+  if (THREADS == 32 && row >= P.rows) return;
+  const int units = P.C / 8;
+  const size_t u0 = (size_t)row * units;
+  float y[UNITS][8];
+#pragma unroll
+  for (int i = 0; i < UNITS; ++i) {
+    const int u = tid + i * THREADS;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[i][e] = 0.0f;
+    if (u < units) load8<DT>(P.x, u0 + u, y[i]);
+  }
+  if (P.residual != nullptr) {
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+      const int u = tid + i * THREADS;
+      if (u < units) {
+        float r[8];
+        load8<DT>(P.residual, u0 + u, r);
+        if constexpr (DT == kBF16) {
+          uint4 s;
+          uint32_t* w = reinterpret_cast<uint32_t*>(&s);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = pack_bf16(y[i][2 * e] + r[2 * e], y[i][2 * e + 1] + r[2 * e + 1]);
+          unpack<DT>(s, y[i]);                           // (the norm is that of the stored sum)
+          if (P.sum != nullptr) P.sum[u0 + u] = s;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[i][e] += r[e];
+          if (P.sum != nullptr) {
+            reinterpret_cast<float4*>(P.sum)[2 * (u0 + u)] = make_float4(y[i][0], y[i][1], y[i][2], y[i][3]);
+            reinterpret_cast<float4*>(P.sum)[2 * (u0 + u) + 1] = make_float4(y[i][4], y[i][5], y[i][6], y[i][7]);
+          }
+        }
+      }
+    }
+  }
+  const auto add = [](float a, float b) { return a + b; };
+  if (P.kind != OVGGT_NORM_NONE) {
+    if (P.kind == OVGGT_NORM_LAYER) {
+      float s = 0.0f;
+#pragma unroll
+      for (int i = 0; i < UNITS; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s += y[i][e];
+      const float mean = row_reduce<THREADS>(s, sh, add) / (float)P.C;
+#pragma unroll
+      for (int i = 0; i < UNITS; ++i)
+        if (tid + i * THREADS < units)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[i][e] -= mean;
+    }
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s = fmaf(y[i][e], y[i][e], s);
+    const float rstd = 1.0f / sqrtf(row_reduce<THREADS>(s, sh, add) / (float)P.C + P.eps);
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+      const int u = tid + i * THREADS;
+      if (u < units) {
+        float w[8];
+        if (P.weight != nullptr) load8<DT>(P.weight, u, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[i][e] *= P.weight != nullptr ? rstd * w[e] : rstd;
+        if (P.bias != nullptr) {
+          load8<DT>(P.bias, u, w);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[i][e] += w[e];
+        }
+      }
+    }
+  }
+  // The maximum of the magnitudes' bits, which order as the magnitudes do, infinities and NaN on top.
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < UNITS; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(y[i][e]) & 0x7FFFFFFFu);
+  most = __reduce_max_sync(0xFFFFFFFFu, most);
+  if constexpr (THREADS > 32)
+    most = __float_as_uint(row_reduce<THREADS>(__uint_as_float(most), sh, [](float a, float b) { return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b))); }));
+  // A row with a value that is not finite gets a scale that is not a number, and products of it are none; a row of
+  // nothing but (almost) zeros a scale of 0: below 2^-119, 127 / maximum has no fp32 value.
+  const float amax = __uint_as_float(most);
+  const bool finite = most < 0x7F800000u, some = finite && amax >= 1.504632769052528e-36f;
+  const float inv = some ? 127.0f / amax : 0.0f;
+#pragma unroll
+  for (int i = 0; i < UNITS; ++i) {
+    const int u = tid + i * THREADS;
+    if (u < units) {
+      float z[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] = some ? fminf(fmaxf(y[i][e] * inv, -127.0f), 127.0f) : 0.0f;
+      P.q[u0 + u] = make_uint2(pack_int8(z[0], z[1], z[2], z[3]), pack_int8(z[4], z[5], z[6], z[7]));
+    }
+  }
+  if (tid == 0) P.scale[row] = some ? amax / 127.0f : (finite ? 0.0f : __int_as_float(0x7FC00000));
+}
+
+constexpr int kNormMaxC = 256 * 8 * 8;
+
+template <int DT>
+static inline cudaError_t norm_q8_launch(const NormQ8Args& P, cudaStream_t st) {
+  const int units = P.C / 8;
+  const auto warp_rows = [&](auto kernel) { return launch_dependent(kernel, dim3((P.rows + kNormWarps - 1) / kNormWarps), kNormWarps * 32, 1, 0, st, true, P); };
+  const auto cta_rows = [&](auto kernel, int threads) { return launch_dependent(kernel, dim3(P.rows), threads, 1, 0, st, true, P); };
+  if (units <= 32) return warp_rows(k_norm_q8<DT, 32, 1>);
+  if (units <= 64) return warp_rows(k_norm_q8<DT, 32, 2>);
+  if (units <= 128) return warp_rows(k_norm_q8<DT, 32, 4>);
+  if (units <= 256) return cta_rows(k_norm_q8<DT, 256, 1>, 256);
+  if (units <= 512) return cta_rows(k_norm_q8<DT, 256, 2>, 256);
+  if (units <= 1024) return cta_rows(k_norm_q8<DT, 256, 4>, 256);
+  return cta_rows(k_norm_q8<DT, 256, 8>, 256);
+}
+
+// ---------------------------------------------------------------- an 8-bit cache: rows in, rows out
+
+// A block is the 64 columns of one row and head.  With 2^e the largest power of two that its largest magnitude reaches (e at least
+// -120, whose step 2^(6 - e) is the last that fp32 holds), the cache has q = round(x 2^(6 - e)), at most 127 in size, and the byte e + 127.  The
+// values q 2^(e - 6) are exact in bf16, so reading back rounds nothing and writing back what was read gives the same
+// bytes.  A block that is not finite is the byte 255, and reads as NaN.
+constexpr int kQ8Lowest = -120;
+
+struct StoreQ8Args {
+  const uint4* src[2];                 // keys, values [seqs, M, C]
+  uint2* q[2];                         // int8 [seqs, cap, C]
+  uint8_t* x[2];                       // [seqs, H, cap]
+  const int* start;                    // [seqs] or nullptr
+  int seqs, M, H, cap;
+};
+
+// Eight lanes a block, eight elements each.
+template <int DT>
+__global__ void __launch_bounds__(256) k_store_q8(const StoreQ8Args P) {
+  pdl_trigger();
+  pdl_wait();
+  const long long at = (long long)blockIdx.x * 256 + threadIdx.x, unit = at >> 3, per_row = P.H;
+  const long long row = unit / per_row;
+  const int h = (int)(unit - row * per_row), part = (int)(at & 7), side = blockIdx.y;
+  const bool in = row < (long long)P.seqs * P.M;
+  const int seq = in ? (int)(row / P.M) : 0, j = in ? (int)(row - (long long)seq * P.M) : 0;
+  const long long to = in ? (P.start != nullptr ? (long long)P.start[seq] : 0) + j : -1;
+  const bool keep = in && (P.start == nullptr || P.start[seq] >= 0) && to < P.cap;
+  float f[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = 0.0f;
+  if (keep) load8<DT>((side == 0 ? P.src[0] : P.src[1]), (size_t)at, f);
+  uint32_t most = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(f[e]) & 0x7FFFFFFFu);
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+  if (!keep) return;
+  const bool finite = most < 0x7F800000u;
+  const int e = max((int)(most >> 23) - 127, kQ8Lowest);
+  const float step = __int_as_float((6 - e + 127) << 23);
+  float z[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) z[i] = finite ? fminf(fmaxf(f[i] * step, -127.0f), 127.0f) : 0.0f;
+  (side == 0 ? P.q[0] : P.q[1])[(((size_t)seq * P.cap + to) * P.H + h) * 8 + part] = make_uint2(pack_int8(z[0], z[1], z[2], z[3]), pack_int8(z[4], z[5], z[6], z[7]));
+  if (part == 0) (side == 0 ? P.x[0] : P.x[1])[((size_t)seq * P.H + h) * P.cap + to] = finite ? (uint8_t)(e + 127) : (uint8_t)255;
+}
+
+struct LoadQ8Args {
+  const uint4* q[2];
+  const uint8_t* x[2];
+  void* dst[2];                        // [seqs, n, C]
+  int seqs, first, n, H, cap;
+};
+
+// 2^(x - 133), the step of a block whose exponent byte is x; NaN for 255.
+__device__ __forceinline__ float q8_step(uint32_t x) { return x == 255u ? __int_as_float(0x7FC00000) : __int_as_float((int)(max(x, 6u) - 6u) << 23); }
+// Byte i of a word of int8 as fp32, exact.
+template <int I>
+__device__ __forceinline__ float int8_at(uint32_t flipped) {   // (flipped: the word ^ 0x80808080)
+  return __uint_as_float(__byte_perm(flipped, 0x4B000000u, 0x7440 + I)) - 8388736.0f;
+}
+
+// Sixteen elements a thread.
+template <int DT>
+__global__ void __launch_bounds__(256) k_load_q8(const LoadQ8Args P) {
+  pdl_trigger();
+  pdl_wait();
+  const long long at = (long long)blockIdx.x * 256 + threadIdx.x, block = at >> 2;
+  const long long row = block / P.H;
+  if (row >= (long long)P.seqs * P.n) return;
+  const int h = (int)(block - row * P.H), seq = (int)(row / P.n), side = blockIdx.y;
+  const int from = P.first + (int)(row - (long long)seq * P.n);
+  const uint4 w = (side == 0 ? P.q[0] : P.q[1])[(((size_t)seq * P.cap + from) * P.H + h) * 4 + (at & 3)];
+  const float step = q8_step((side == 0 ? P.x[0] : P.x[1])[((size_t)seq * P.H + h) * P.cap + from]);
+  float f[16];
+  const uint32_t u[4] = {w.x ^ 0x80808080u, w.y ^ 0x80808080u, w.z ^ 0x80808080u, w.w ^ 0x80808080u};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[4 * i] = int8_at<0>(u[i]) * step;
+    f[4 * i + 1] = int8_at<1>(u[i]) * step;
+    f[4 * i + 2] = int8_at<2>(u[i]) * step;
+    f[4 * i + 3] = int8_at<3>(u[i]) * step;
+  }
+  if constexpr (DT == kBF16) {
+    uint32_t o[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = pack_bf16(f[2 * i], f[2 * i + 1]);
+    uint4* d = static_cast<uint4*>(side == 0 ? P.dst[0] : P.dst[1]) + 2 * (size_t)at;
+    d[0] = make_uint4(o[0], o[1], o[2], o[3]);
+    d[1] = make_uint4(o[4], o[5], o[6], o[7]);
+  } else {
+    float4* d = static_cast<float4*>(side == 0 ? P.dst[0] : P.dst[1]) + 4 * (size_t)at;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) d[i] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+  }
+}
+
+}  // namespace ovggt

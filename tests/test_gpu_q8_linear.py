@@ -1,0 +1,96 @@
+"""The int8 product: its sums are exact, so its bits are those of the formula in fp32, at every size and split."""
+import pytest
+import torch
+
+from paper_2603_05959_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+# rows, columns, K: one token to frames, partial tiles on each side, K that ends inside a tile
+SHAPES = [(1, 8, 16), (1, 4096, 1024), (2, 24, 48), (5, 1024, 4096), (7, 72, 80), (8, 264, 528), (9, 136, 64), (16, 768, 1040), (17, 48, 112), (33, 512, 2048),
+          (64, 1024, 1024), (65, 128, 256), (127, 72, 64), (128, 256, 128), (129, 264, 192), (333, 512, 2064), (718, 2304, 768), (1041, 1024, 4096),
+          (1374, 4096, 1024), (2049, 40, 16)]
+
+
+def _case(M, N, K, seed=0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(M + N + K + seed)
+    a = torch.randint(-127, 128, (M, K), generator=g, device="cuda").to(torch.int8)
+    w = torch.randint(-128, 128, (N, K), generator=g, device="cuda").to(torch.int8)
+    as_, ws = (torch.rand(n, generator=g, device="cuda") * 0.02 / K ** 0.5 for n in (M, N))
+    x = torch.randn((M, N), generator=g, device="cuda").bfloat16()
+    return a, as_, w, ws, x, torch.zeros(16, dtype=torch.int32, device="cuda")
+
+
+def _t(a, as_, w, ws):
+    # (products of whole numbers: exact in 64 bits; rounded to fp32, scaled by the token's and then the channel's, to bf16)
+    return ((a.double() @ w.double().T).float() * as_[:, None] * ws).bfloat16()
+
+
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_linear(M, N, K):
+    a, as_, w, ws, x, st = _case(M, N, K)
+    ws = ws * 400                                        # (products of about one: GELU's middle)
+    ref = _t(a, as_, w, ws)
+    t, s = torch.empty_like(x), torch.empty_like(x)
+    B.k_linear_q8(a, as_, w, ws, (t,), residual=x, sum_out=s, status=st)
+    assert torch.equal(t, ref) and torch.equal(s, x + ref)
+    s.zero_()
+    B.k_linear_q8(a, as_, w, ws, (), residual=x, sum_out=s, status=st)
+    assert torch.equal(s, x + ref)
+    B.k_linear_q8(a, as_, w, ws, (), residual=x, sum_out=x, status=st)
+    assert torch.equal(s, x)                             # (the residual stream in place)
+    B.k_linear_q8(a, as_, w, ws, (t,), gelu=True, status=st)
+    assert torch.equal(t, torch.nn.functional.gelu(ref))
+    for n in (2, 3):
+        if N % (8 * n) == 0:
+            parts = [torch.empty((M, N // n), dtype=torch.bfloat16, device="cuda") for _ in range(n)]
+            B.k_linear_q8(a, as_, w, ws, parts, status=st)
+            assert torch.equal(torch.cat(parts, 1), ref)
+    assert int(st[0]) == 0
+
+
+@pytest.mark.parametrize("M", [1, 40, 700])
+def test_largest_sums(M):
+    """The longest K: every product -128 x -128, and the sum stays within int32."""
+    K = 131056
+    a = torch.full((M, K), -128, dtype=torch.int8, device="cuda")
+    w = torch.full((8, K), -128, dtype=torch.int8, device="cuda")
+    one = torch.ones(M, device="cuda")
+    t = torch.empty((M, 8), dtype=torch.bfloat16, device="cuda")
+    st = torch.zeros(16, dtype=torch.int32, device="cuda")
+    B.k_linear_q8(a, one, w, torch.ones(8, device="cuda"), (t,), status=st)
+    assert torch.equal(t, torch.full_like(t, float(16384 * K)))
+
+
+@pytest.mark.parametrize("M", [3, 300])
+def test_scales_that_are_not_finite(M):
+    a, as_, w, ws, x, st = _case(M, 64, 64)
+    as_[1], ws[5] = float("nan"), float("inf")
+    t = torch.empty((M, 64), dtype=torch.bfloat16, device="cuda")
+    B.k_linear_q8(a, as_, w, ws, (t,), status=st)
+    ref = _t(a, as_, w, ws)
+    assert torch.equal(t.isnan(), ref.isnan()) and torch.equal(t.nan_to_num(), ref.nan_to_num())
+    assert bool(t[1].isnan().all()) and not bool(t[0, :5].isnan().any())
+
+
+@pytest.mark.parametrize("M", [5, 300])
+def test_rows_behind_the_last_are_left_alone(M):
+    a, as_, w, ws, _, st = _case(M, 72, 80)
+    whole = torch.full((M + 200, 72), 7.0, dtype=torch.bfloat16, device="cuda")
+    B.k_linear_q8(a, as_, w, ws, (whole[:M],), status=st)
+    assert torch.equal(whole[:M], _t(a, as_, w, ws)) and bool((whole[M:] == 7).all())
+
+
+def test_arguments():
+    a, as_, w, ws, x, st = _case(16, 32, 64)
+    t = torch.empty_like(x)
+    ok = dict(a=a, a_scale=as_, w=w, w_scale=ws, outs=(t,), residual=x, sum_out=torch.empty_like(x), status=st)
+    B.k_linear_q8(**ok)
+    for over in (dict(a=a.float()), dict(w=w.float()), dict(a=a[:, :48].contiguous()), dict(a_scale=as_[:8]), dict(w_scale=ws.double()),
+                 dict(outs=(t.float(),)), dict(outs=(t[:8],)), dict(residual=x[:8]), dict(sum_out=x.float()), dict(outs=(t,) * 4),
+                 dict(w=w.T.contiguous().T)):
+        with pytest.raises(AssertionError):
+            B.k_linear_q8(**dict(ok, **over))
+    with pytest.raises(B.OvggtError):
+        B.k_linear_q8(**dict(ok, residual=None))
