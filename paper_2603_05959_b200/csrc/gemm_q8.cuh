@@ -29,9 +29,10 @@ __device__ __forceinline__ void q8_finish8(const GemmQ8Args& P, int m, int n, co
   uint32_t w[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) w[e] = pack_bf16((float)acc[2 * e] * as * s[2 * e], (float)acc[2 * e + 1] * as * s[2 * e + 1]);
-  if (P.o.gelu)
+  if (P.o.gelu) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) w[e] = pack_bf16(gelu(__uint_as_float(w[e] << 16)), gelu(__uint_as_float(w[e] & 0xFFFF0000u)));
+  }
   const uint4 t = make_uint4(w[0], w[1], w[2], w[3]);
   if (P.o.residual != nullptr)
     gemm_store8<true>(P.o, m, n, t, *reinterpret_cast<const uint4*>(P.o.residual + (size_t)m * P.o.N + n));
@@ -92,8 +93,238 @@ __global__ void __launch_bounds__(256) k_linear_q8_few(const GemmQ8Args P) {
   }
 }
 
+// ---------------------------------------------------------------- many tokens: tcgen05
+//
+// A persistent CTA per SM takes tiles of 128 tokens x BN channels (256, 128 or 64) in turn.  K in steps of 128: A [128, 128] and W [BN, 128], both
+// K-major in 128-byte swizzled rows as they lie in memory, 32 columns of K an MMA, int32 sums in BN of 2 BN TMEM columns: while the epilogue
+// warps take one tile's sums, the MMAs of the next tile run.
+//   warps 0-15  epilogue: 32 tokens and a quarter of the channels each, 32 channels (64 or 128 wide tiles: 16 or 32) at a time, through 2 KB of
+//               shared memory into whole sectors
+//   warp 16     TMA producer; warp 17 allocates tensor memory and issues the MMAs
+// Every wait is bounded, as in the bf16 product.
+constexpr int kQ8K = 128, kQ8ATile = 128 * kQ8K;
+__host__ __device__ constexpr int q8_stage_bytes(int bn) { return kQ8ATile + bn * kQ8K; }
+__host__ __device__ constexpr int q8_stages(int bn) { return bn == 256 ? 4 : (bn == 128 ? 6 : 8); }
+__host__ __device__ constexpr int q8_chunk(int bn) { return bn >= 128 ? 32 : 16; }        // channels of a warp at a time
+__host__ __device__ constexpr int q8_staging(int bn) { return kGemmEpilogueWarps * 32 * q8_chunk(bn) * 2; }
+constexpr int kQ8MaxStages = 8;
+
+struct Q8Barriers {
+  unsigned long long full[kQ8MaxStages], empty[kQ8MaxStages], acc_full[2], acc_empty[2], drain;
+  uint32_t tmem_base;
+  int abort_flag;
+};
+__host__ __device__ constexpr size_t q8_smem_bytes(int bn) {
+  return (size_t)q8_stages(bn) * q8_stage_bytes(bn) + q8_staging(bn) + sizeof(Q8Barriers) + 64;
+}
+
+// Instruction descriptor: int8 x int8 -> int32, both K-major, M = 128.
+__host__ __device__ constexpr uint32_t idesc_s8(int n) { return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24); }
+
+__device__ __forceinline__ void mma_ss_s8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n}\n" ::"r"(d_tmem), "l"(a_desc), "l"(b_desc),
+      "r"(idesc), "r"(acc)
+      : "memory");
+}
+
+// GELU and the residual's sum in instances of their own.
+template <int BN, bool GELU, bool RES>
+__global__ void __launch_bounds__(kGemmThreads, 1)
+k_linear_q8_tcgen05(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ GemmQ8Args P) {
+  constexpr int kStages = q8_stages(BN), kStage = q8_stage_bytes(BN);
+  constexpr int kProducer = kGemmEpilogueWarps, kIssuer = kGemmEpilogueWarps + 1;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  unsigned char* staging = smem + kStages * kStage;
+  Q8Barriers* B = reinterpret_cast<Q8Barriers*>(staging + q8_staging(BN));
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int k_tiles = (P.o.K + kQ8K - 1) / kQ8K, tiles_m = (P.o.M + 127) / 128, tiles_n = (P.o.N + BN - 1) / BN;
+  const int tiles = tiles_m * tiles_n;
+  const bool aligned = (smem_u32(smem) & 1023u) == 0;
+  if (!aligned && threadIdx.x == 0) report_status(P.o.status, OVGGT_ERR_DEVICE_STATUS);
+  pdl_trigger();
+
+  if (warp == kProducer && lane == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_a) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_w) : "memory");
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&B->full[s], 1);
+      mbar_init(&B->empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&B->acc_full[b], 1);
+      mbar_init(&B->acc_empty[b], kGemmEpilogueWarps);
+    }
+    mbar_init(&B->drain, 1);
+    B->abort_flag = aligned ? 0 : 1;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    // the weights of its first tile, into L2 while the kernel before drains: a share of them with the CTAs of the same channels
+    if ((int)blockIdx.x < tiles)
+      for (int kt = (int)blockIdx.x % tiles_m; kt < k_tiles; kt += tiles_m) tma_prefetch_2d(&tm_w, kt * (kQ8K / 2), (int)blockIdx.x / tiles_m * BN);
+  }
+  if (warp == kIssuer) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&B->tmem_base)), "r"((uint32_t)(2 * BN)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *(volatile uint32_t*)&B->tmem_base;
+  pdl_wait();
+
+  bool ok = aligned;
+  if (warp == kProducer) {
+    // ------------------------------------------------ TMA producer
+    if (lane == 0) {
+      int issued = 0;
+      for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
+        const int m0 = tile % tiles_m * 128, n0 = tile / tiles_m * BN;
+        for (int kt = 0; kt < k_tiles; ++kt, ++issued) {
+          const int s = issued % kStages;
+          if (issued >= kStages) ok = mbar_wait(&B->empty[s], (uint32_t)(issued / kStages - 1) & 1u, B, P.o.status);
+          if (!ok) break;
+          unsigned char* st = smem + s * kStage;
+          mbar_expect_tx(&B->full[s], kStage);
+          tma_load_2d(st, &tm_a, kt * (kQ8K / 2), m0, &B->full[s]);
+          tma_load_2d(st + kQ8ATile, &tm_w, kt * (kQ8K / 2), n0, &B->full[s]);
+        }
+      }
+      if (!ok)   // leave no bulk copy in flight into this CTA's shared memory
+        for (int i = max(0, issued - kStages); i < issued; ++i)
+          mbar_wait(&B->full[i % kStages], (uint32_t)(i / kStages) & 1u, B, P.o.status);
+    }
+    __syncwarp();
+  } else if (warp == kIssuer) {
+    // ------------------------------------------------ MMA issuer (whole warp in step, one elected lane issues)
+    const bool leader = elect_one();
+    const uint32_t tm = __reduce_or_sync(0xFFFFFFFFu, tmem);
+    constexpr uint32_t idesc = idesc_s8(BN);
+    auto wait_all = [&](void* bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, B, P.o.status)) != 0; };
+    int it = 0, j = 0;
+    for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x, ++j) {
+      const int buf = j & 1;
+      if (j >= 2) ok = wait_all(&B->acc_empty[buf], (uint32_t)(j / 2 - 1) & 1u);
+      if (!ok) break;
+      tc_fence_after();
+      for (int kt = 0; kt < k_tiles; ++kt, ++it) {
+        const int s = it % kStages;
+        ok = wait_all(&B->full[s], (uint32_t)(it / kStages) & 1u);
+        if (!ok) break;
+        tc_fence_after();
+        const uint64_t da = smem_desc_sw128(smem_u32(smem + s * kStage)), dw = smem_desc_sw128(smem_u32(smem + s * kStage + kQ8ATile));
+        if (leader) {
+#pragma unroll
+          for (int kk = 0; kk < kQ8K / 32; ++kk)
+            mma_ss_s8(tm + buf * BN, da + (uint64_t)(kk * 2), dw + (uint64_t)(kk * 2), idesc, (kt > 0 || kk > 0));
+          tc_commit(&B->empty[s]);
+          if (kt + 1 == k_tiles) tc_commit(&B->acc_full[buf]);
+        }
+      }
+    }
+    if (aligned) {
+      if (leader) tc_commit(&B->drain);               // every issued MMA finishes before TMEM is freed
+      wait_all(&B->drain, 0);
+    }
+    __syncwarp();
+  } else {
+    // ------------------------------------------------ epilogue
+    constexpr int kCols = BN / 4, kChunk = q8_chunk(BN), kUnits = kChunk / 8;     // a warp's channels, those of a round, their 16-byte units
+    const int quad = warp & 3, side = warp >> 2;
+    uint4* stage = reinterpret_cast<uint4*>(staging) + warp * 32 * kUnits;
+    int j = 0;
+    for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x, ++j) {
+      const int buf = j & 1, row0 = tile % tiles_m * 128 + quad * 32, col0 = tile / tiles_m * BN + side * kCols;
+      const float as = row0 + lane < P.o.M ? P.a_scale[row0 + lane] : 0.0f;
+      ok = __all_sync(0xFFFFFFFFu, mbar_wait(&B->acc_full[buf], (uint32_t)(j / 2) & 1u, B, P.o.status)) != 0;
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t t_row = tmem + ((uint32_t)(quad * 32) << 16) + buf * BN + side * kCols;
+#pragma unroll 1
+      for (int c = 0; c < kCols; c += kChunk) {
+        const int col = col0 + c;
+        uint4 res[RES ? kUnits : 1];
+        if constexpr (RES) {
+#pragma unroll
+          for (int i = 0; i < kUnits; ++i) {
+            const int r = row0 + (lane + 32 * i) / kUnits, n = col + (lane + 32 * i) % kUnits * 8;
+            if (r < P.o.M && n < P.o.N) res[i] = *reinterpret_cast<const uint4*>(P.o.residual + (size_t)r * P.o.N + n);
+          }
+        }
+#pragma unroll
+        for (int h = 0; h < kChunk; h += 16) {
+          uint32_t o[16];
+          tmem_ld16(t_row + c + h, o);
+          tmem_wait_ld();
+          if (c + kChunk >= kCols && h + 16 >= kChunk) {                      // the last of this tile's sums: the buffer is free
+            tc_fence_before();
+            if (lane == 0) mbar_arrive(&B->acc_empty[buf]);
+          }
+          uint32_t w[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {                                        // (N a multiple of 8: scales past it are not read)
+            const int n = col + h + 4 * e;
+            const float4 ws = n < P.o.N ? __ldg(reinterpret_cast<const float4*>(P.w_scale + n)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            w[2 * e] = pack_bf16((float)(int)o[4 * e] * as * ws.x, (float)(int)o[4 * e + 1] * as * ws.y);
+            w[2 * e + 1] = pack_bf16((float)(int)o[4 * e + 2] * as * ws.z, (float)(int)o[4 * e + 3] * as * ws.w);
+          }
+          if constexpr (GELU) gelu_warp(w);
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+            stage[lane * kUnits + ((h / 8 + u) ^ (lane & (kUnits - 1)))] = make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+          const int r = (lane + 32 * i) / kUnits, u = (lane + 32 * i) % kUnits;
+          if (row0 + r < P.o.M && col + u * 8 < P.o.N)
+            gemm_store8<RES>(P.o, row0 + r, col + u * 8, stage[r * kUnits + (u ^ (r & (kUnits - 1)))], res[RES ? i : 0]);
+        }
+        __syncwarp();
+      }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kIssuer) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)(2 * BN)) : "memory");
+  }
+}
+
+template <int BN>
+static inline int q8_tcgen05_launch(const GemmQ8Args& P, cudaStream_t st) {
+  CUtensorMap ta, tw;
+  // (128 int8 columns as 64 of two bytes: the copies move bits)
+  int rc = make_rows_map(&ta, P.a, P.o.M, P.o.K / 2, 128);
+  if (rc) return rc;
+  rc = make_rows_map(&tw, P.w, P.o.N, P.o.K / 2, BN);
+  if (rc) return rc;
+  const bool gelu = P.o.gelu != 0, res = P.o.residual != nullptr;
+  const auto kernel = gelu ? (res ? k_linear_q8_tcgen05<BN, true, true> : k_linear_q8_tcgen05<BN, true, false>)
+                           : (res ? k_linear_q8_tcgen05<BN, false, true> : k_linear_q8_tcgen05<BN, false, false>);
+  static std::atomic<uint64_t> smem_set[4];
+  cudaError_t e = allow_smem(kernel, q8_smem_bytes(BN), smem_set[2 * gelu + res]);
+  const long tiles = (long)((P.o.M + 127) / 128) * ((P.o.N + BN - 1) / BN);
+  if (tiles > 0x7FFF0000) return OVGGT_ERR_UNSUPPORTED;
+  if (e == cudaSuccess) e = launch_dependent(kernel, dim3((unsigned)std::min(tiles, 148l)), kGemmThreads, 1, q8_smem_bytes(BN), st, true, ta, tw, P);
+  if (e != cudaSuccess) { g_attn_last_error = (int)e; return OVGGT_ERR_CUDA; }
+  return OVGGT_OK;
+}
+
+constexpr int kQ8Few = 32;             // tokens up to which the few-token kernel is taken
+
 static inline int gemm_q8_launch(const GemmQ8Args& P, cudaStream_t st) {
-  const int M = P.o.M, groups = M <= 8 ? 1 : (M <= 16 ? 2 : 4);
+  const int M = P.o.M;
+  if (M > kQ8Few) {
+    const long tiles_m = (M + 127) / 128;
+    if (tiles_m * ((P.o.N + 255) / 256) >= 148) return q8_tcgen05_launch<256>(P, st);
+    if (tiles_m * ((P.o.N + 127) / 128) >= 100) return q8_tcgen05_launch<128>(P, st);
+    return q8_tcgen05_launch<64>(P, st);
+  }
+  const int groups = M <= 8 ? 1 : (M <= 16 ? 2 : 4);
   const auto kernel = groups == 1 ? k_linear_q8_few<1> : (groups == 2 ? k_linear_q8_few<2> : k_linear_q8_few<4>);
   const cudaError_t e = launch_dependent(kernel, dim3((P.o.N + 15) / 16, (M + 8 * groups - 1) / (8 * groups)), 256, 1, 0, st, true, P);
   if (e != cudaSuccess) { g_attn_last_error = (int)e; return OVGGT_ERR_CUDA; }

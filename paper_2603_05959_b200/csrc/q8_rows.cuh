@@ -108,9 +108,10 @@ __global__ void __launch_bounds__(THREADS == 32 ? kNormWarps * 32 : THREADS) k_n
       const float mean = row_reduce<THREADS>(s, sh, add) / (float)P.C;
 #pragma unroll
       for (int i = 0; i < UNITS; ++i)
-        if (tid + i * THREADS < units)
+        if (tid + i * THREADS < units) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) y[i][e] -= mean;
+        }
     }
     float s = 0.0f;
 #pragma unroll

@@ -9,7 +9,7 @@ pytestmark = pytest.mark.gpu
 # rows, columns, K: one token to frames, partial tiles on each side, K that ends inside a tile
 SHAPES = [(1, 8, 16), (1, 4096, 1024), (2, 24, 48), (5, 1024, 4096), (7, 72, 80), (8, 264, 528), (9, 136, 64), (16, 768, 1040), (17, 48, 112), (33, 512, 2048),
           (64, 1024, 1024), (65, 128, 256), (127, 72, 64), (128, 256, 128), (129, 264, 192), (333, 512, 2064), (718, 2304, 768), (1041, 1024, 4096),
-          (1374, 4096, 1024), (2049, 40, 16)]
+          (1374, 4096, 1024), (2049, 40, 16), (4500, 1032, 272), (20000, 520, 144), (30001, 72, 48)]
 
 
 def _case(M, N, K, seed=0):
