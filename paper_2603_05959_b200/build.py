@@ -53,7 +53,7 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False) -> 
     if r.returncode != 0:
         raise subprocess.CalledProcessError(r.returncode, cmd)
     try:
-        for kernel in ("k_attn_tcgen05", "k_attn_f32"):
+        for kernel in ("k_attn_tcgen05", "k_attn_f32", "k_attn_q8_many"):
             check_register_pool(r.stdout, kernel)
     except Exception:
         os.remove(tmp)

@@ -342,8 +342,449 @@ __global__ void __launch_bounds__(kFewWarps * 32) k_attn_q8_few(const AttnQ8Args
   if (S > 1) cluster.sync();                             // (nobody leaves while its part is being read)
 }
 
+// ---------------------------------------------------------------- many rows: tcgen05, the cache widened on its way into shared memory
+//
+// The bf16 attention's scheme (see attn_tcgen05.cuh: halves of 96 cached rows with a buffer of scores each, so that the MMAs of one half run
+// under the softmax of the other) for two tiles of 128 rows a CTA, whose K and V tiles six warps read as int8 and write as bf16 planes, once
+// for both: q 2^(x - 133) is exact in bf16, so the operands are what the cache stands for.  A plane costs 2.5 instructions an element,
+// shared by 256 rows; a pass of its own that writes bf16 planes to memory would move 5 bytes an element instead of one.
+//   warps 0-7    softmax, four a tile, one thread a row; the running maximum moves when it is outgrown by 2^8 and O is rescaled then
+//   warps 8, 9   MMA issuers, one a tile; warp 8 allocates tensor memory (2 x 256 columns)
+//   warps 10-15  K and V: copied to shared memory two tiles ahead, widened there
+// The cached rows of a sequence and head are shared out over a cluster of CTAs, whose parts are joined through distributed shared memory.
+// Every wait is bounded; on expiry the CTA records OVGGT_ERR_TIMEOUT and leaves through the common teardown.
+constexpr int kManyThreads = 512, kManyConverters = 192, kManyRows = 2 * kBM;
+constexpr int kManyRegsSoftmax = 200, kManyRegsOther = 56;
+static_assert(256 * kManyRegsSoftmax + 256 * kManyRegsOther <= kManyThreads * kRegsLaunch, "register pool of the CTA exceeded");
+constexpr int kManyPitch = kHD + 4;                      // floats between the rows of O in shared memory
+
+struct ManyBarriers {
+  unsigned long long k_full[kKVStages], k_empty[kKVStages], v_full[kKVStages], v_empty[kKVStages];
+  unsigned long long s_full[2][2], p_full[2][2], pv_done[2], o_full[2], drain[2];   // by row tile
+  uint32_t tmem_base;
+  int abort_flag;
+};
+constexpr int kManyRaw = 3, kManyRawStage = 2 * kBN * kHD;   // stages of K and V tiles as they lie in the cache; O, maxima and sums come to lie over them
+constexpr int kManyO = 2 * kQBytes + 2 * kKVStages * kTileBytes;
+constexpr int kManyBar = kManyO + kManyRaw * kManyRawStage;
+static_assert(kManyRows * (kManyPitch + 2) * 4 <= kManyRaw * kManyRawStage, "a CTA's result does not fit the tiles it lies over");
+constexpr int kManySmem = kManyBar + (int)sizeof(ManyBarriers);
+
+// 2^(x - 133) as a pair of bf16; NaN for 255.
+__device__ __forceinline__ uint32_t q8_step_bf16x2(uint32_t x) { return (x == 255u ? 0x7FFFu : (max(x, 6u) - 6u) << 7) * 0x00010001u; }
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  const __nv_bfloat162 d = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&d);
+}
+// 16 int8 of columns [16 c, 16 c + 16) of row r, times step -> the same place of a swizzled bf16 tile.
+__device__ __forceinline__ void store_widened(unsigned char* tile, int r, int c, const uint4& w, uint32_t step) {
+  const uint32_t in[4] = {w.x, w.y, w.z, w.w};
+  uint32_t o[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    o[2 * i] = mul_bf16x2(int8_to_bf16x2(__byte_perm(in[i], 0x43434343u, 0x4140)), step);
+    o[2 * i + 1] = mul_bf16x2(int8_to_bf16x2(__byte_perm(in[i], 0x43434343u, 0x4342)), step);
+  }
+  unsigned char* p = tile + r * 128;
+  *reinterpret_cast<uint4*>(p + (((2 * c) ^ (r & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+  *reinterpret_cast<uint4*>(p + (((2 * c + 1) ^ (r & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+}
+
+__global__ void __launch_bounds__(kManyThreads, 1) k_attn_q8_many(const __grid_constant__ AttnQ8Args P) {
+  namespace cg = cooperative_groups;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int S = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const bool aligned = (smem_u32(smem) & 1023u) == 0;    // the 128-byte swizzle needs 1024-byte aligned tiles
+  if (!aligned && threadIdx.x == 0) report_status(P.status, OVGGT_ERR_DEVICE_STATUS);
+  unsigned char* sQ = smem;
+  unsigned char* sK = sQ + 2 * kQBytes;
+  unsigned char* sV = sK + kKVStages * kTileBytes;
+  unsigned char* sRaw = smem + kManyO;
+  float* sO = reinterpret_cast<float*>(sRaw);            // [256][kManyPitch], then maxima [256], sums [256], once every tile has been widened
+  ManyBarriers* B = reinterpret_cast<ManyBarriers*>(smem + kManyBar);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long job = blockIdx.x / S;
+  const int hk = (int)(job % P.HK), qt = (int)(job / P.HK % P.q_tiles), seq = (int)(job / P.HK / P.q_tiles);
+  const int rows = P.M * P.group, row0 = qt * kManyRows, n_q = min(2, (rows - row0 + kBM - 1) / kBM);   // row tiles of this CTA
+  auto q_at = [&](int r) {                               // (row r is token r / group, head r % group of this group)
+    const int m = r / P.group;
+    return (((size_t)seq * P.M + m) * P.H + (size_t)hk * P.group + (r - m * P.group)) * kHD;
+  };
+  pdl_trigger();
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kKVStages; ++s) {
+      mbar_init(&B->k_full[s], kManyConverters);
+      mbar_init(&B->v_full[s], kManyConverters);
+      mbar_init(&B->k_empty[s], n_q);
+      mbar_init(&B->v_empty[s], n_q);
+    }
+    for (int i = 0; i < 2; ++i) {
+      for (int hf = 0; hf < 2; ++hf) {
+        mbar_init(&B->s_full[i][hf], 1);
+        mbar_init(&B->p_full[i][hf], 128);
+      }
+      mbar_init(&B->pv_done[i], 1);
+      mbar_init(&B->o_full[i], 1);
+      mbar_init(&B->drain[i], 1);
+    }
+    B->abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&B->tmem_base)), "r"((uint32_t)(2 * kTmemCols)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  pdl_wait();
+  const int len = min(P.cap, max(0, P.lens != nullptr ? P.lens[seq] : P.cap));
+  const int tiles_total = (len + kBN - 1) / kBN;
+  const int t_begin = (int)((long long)rank * tiles_total / S), n_tiles = aligned ? (int)((long long)(rank + 1) * tiles_total / S) - t_begin : 0;
+  {                                                      // Q: 256 rows x 8 groups of 8 columns, rows past the last zero
+    constexpr int kPer = kManyRows * 8 / kManyThreads;
+    uint4 x[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int idx = threadIdx.x + i * kManyThreads, r = row0 + (idx >> 3);
+      x[i] = r < rows ? *reinterpret_cast<const uint4*>(P.q + q_at(r) + (idx & 7) * 8) : make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int idx = threadIdx.x + i * kManyThreads, r = idx >> 3;
+      *reinterpret_cast<uint4*>(sQ + r * 128 + (((idx & 7) ^ (r & 7)) << 4)) = x[i];
+    }
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *(volatile uint32_t*)&B->tmem_base;
+  // Every warp of the cluster meets here at the end, each in its own branch: what follows a change of registers stays in it.
+  auto sync_all = [&]() {
+    __syncwarp();
+    if (S > 1) cluster.sync(); else asm volatile("barrier.sync.aligned 0;" ::: "memory");
+  };
+
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kManyRegsOther));
+    if (warp < 10) {
+      // ------------------------------------------------ MMA issuers, in the bf16 attention's order:
+      // QK(0,0) QK(0,1) | PV(0,0) QK(1,0) PV(0,1) QK(1,1) | PV(1,0) QK(2,0) ...
+      const int i = warp - 8;
+      if (i < n_q && n_tiles > 0) {
+        const bool leader = elect_one();
+        const uint32_t tm = __reduce_or_sync(0xFFFFFFFFu, tmem) + i * kTmemCols;
+        constexpr uint32_t idesc_qk = idesc_bf16(kHalf, false), idesc_pv = idesc_bf16(kHD, true);
+        const uint64_t dq = smem_desc_sw128(smem_u32(sQ + i * kQBytes));
+        auto wait_all = [&](void* bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, B, P.status)) != 0; };
+        auto issue_qk = [&](int st, int hf) {
+          const uint64_t dk = smem_desc_sw128(smem_u32(sK + st * kTileBytes + hf * (kTileBytes / 2)));
+          if (leader) {
+#pragma unroll
+            for (int kk = 0; kk < kHD / 16; ++kk) mma_ss(tm + kColS + hf * kHalf, dq + (uint64_t)(kk * 2), dk + (uint64_t)(kk * 2), idesc_qk, kk > 0);
+            tc_commit(&B->s_full[i][hf]);
+            if (hf == 1) tc_commit(&B->k_empty[st]);
+          }
+        };
+        bool ok = wait_all(&B->k_full[0], 0);
+        if (ok) {
+          tc_fence_after();
+          issue_qk(0, 0);
+          issue_qk(0, 1);
+        }
+        for (int it = 0; it < n_tiles && ok; ++it) {
+          const int s = it % kKVStages, s1 = (it + 1) % kKVStages;
+          const uint32_t ph = (uint32_t)(it / kKVStages) & 1u, ph1 = (uint32_t)((it + 1) / kKVStages) & 1u;
+          const bool more = it + 1 < n_tiles;
+          ok = wait_all(&B->v_full[s], ph);
+          if (!ok) break;
+          const uint64_t dv = smem_desc_sw128(smem_u32(sV + s * kTileBytes));
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            ok = wait_all(&B->p_full[i][hf], (uint32_t)it & 1u);
+            if (!ok) break;
+            tc_fence_after();
+            if (leader) {
+#pragma unroll
+              for (int kk = 0; kk < kHalf / 16; ++kk)
+                mma_ts(tm + kColO, tm + kColS + hf * kHalf + kk * 8, dv + (uint64_t)((hf * (kHalf / 16) + kk) * 128), idesc_pv, (it > 0 || hf > 0 || kk > 0));
+              if (hf == 1) tc_commit(&B->v_empty[s]);
+              if (!more && hf == 0) tc_commit(&B->pv_done[i]);   // (the last half has no later score MMA to tell it by)
+            }
+            if (more) {
+              if (hf == 0) {
+                ok = wait_all(&B->k_full[s1], ph1);
+                if (!ok) break;
+                tc_fence_after();
+              }
+              issue_qk(s1, hf);
+            }
+          }
+        }
+        if (ok) {
+          if (leader) tc_commit(&B->o_full[i]);
+          wait_all(&B->o_full[i], 0);
+        } else {
+          if (leader) tc_commit(&B->drain[i]);           // let every issued MMA finish before TMEM is freed
+          wait_all(&B->drain[i], 0);
+        }
+      }
+      __syncwarp();
+    } else if (n_tiles > 0) {
+      // ------------------------------------------------ K and V
+      // A thread has four adjacent rows of a tile, 16 columns of each, and reads back what it copied itself: no barrier between the copy
+      // and the widening.  (Two threads next to each other take their rows in another order: their stores go to different banks.)
+      const int ct = (int)threadIdx.x - 320, c = ct & 3, g = ct >> 2;
+      const size_t pitch = (size_t)P.HK * kHD, base = ((size_t)seq * P.cap * P.HK + hk) * kHD + c * 16, xbase = ((size_t)seq * P.HK + hk) * P.cap;
+      auto request = [&](int t) {
+        if (t < n_tiles) {
+          unsigned char* raw = sRaw + (t % kManyRaw) * kManyRawStage + ct * 16;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int r = (t_begin + t) * kBN + 4 * g + (i ^ (g & 1));
+            const size_t at = base + (size_t)min(r, len - 1) * pitch;
+            copy16(raw + i * (kManyConverters * 16), P.kq + at, r < len);
+            copy16(raw + (4 + i) * (kManyConverters * 16), P.vq + at, r < len);
+          }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      };
+      struct Bytes { uint32_t k, v, live; };               // of the four rows
+      auto bytes_of = [&](int t) {
+        const int r = (t_begin + t) * kBN + 4 * g;         // (the capacity is a multiple of 16)
+        Bytes b = {0u, 0u, 0xFFFFFFFFu};
+        if (t < n_tiles && r < len) {
+          b.k = __ldg(reinterpret_cast<const uint32_t*>(P.kx + xbase + r));
+          b.v = __ldg(reinterpret_cast<const uint32_t*>(P.vx + xbase + r));
+          if (P.live != nullptr) b.live = __ldg(reinterpret_cast<const uint32_t*>(P.live + (size_t)seq * P.cap + r));
+        }
+        return b;
+      };
+      auto widen = [&](bool values, int t, const Bytes& b, unsigned char* tiles) {
+        const unsigned char* raw = sRaw + (t % kManyRaw) * kManyRawStage + (values ? 4 : 0) * (kManyConverters * 16) + ct * 16;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int e = i ^ (g & 1), r = 4 * g + e;
+          uint32_t x = b.k >> (8 * e) & 255u;
+          // a row that is masked counts for nothing; one whose key is not finite makes the result NaN whatever its weight came out as
+          if (values) x = (b.live >> (8 * e) & 255u) == 0u ? 0u : (x == 255u ? 255u : b.v >> (8 * e) & 255u);
+          if ((t_begin + t) * kBN + r >= len) x = 0u;
+          store_widened(tiles + t % kKVStages * kTileBytes, r, c, *reinterpret_cast<const uint4*>(raw + i * (kManyConverters * 16)), q8_step_bf16x2(x));
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      };
+#pragma unroll
+      for (int t = 0; t < kManyRaw - 1; ++t) request(t);
+      Bytes next = bytes_of(0);
+#pragma unroll 1
+      for (int t = 0; t < n_tiles; ++t) {
+        const Bytes b = next;
+        next = bytes_of(t + 1);
+        request(t + kManyRaw - 1);
+        asm volatile("cp.async.wait_group %0;" ::"n"(kManyRaw - 1) : "memory");
+        const int s = t % kKVStages;
+        const uint32_t ph = (uint32_t)(t / kKVStages - 1) & 1u;
+        if (t >= kKVStages && !mbar_wait(&B->k_empty[s], ph, B, P.status)) break;
+        widen(false, t, b, sK);
+        mbar_arrive(&B->k_full[s]);
+        if (t >= kKVStages && !mbar_wait(&B->v_empty[s], ph, B, P.status)) break;
+        widen(true, t, b, sV);
+        mbar_arrive(&B->v_full[s]);
+      }
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
+      __syncwarp();
+    }
+    // ---- teardown: the softmax warps join the parts
+    tc_fence_before();
+    sync_all();
+    if (warp == 8) {
+      tc_fence_after();
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)(2 * kTmemCols)) : "memory");
+    }
+    if (S > 1) sync_all();
+  } else {
+    // ------------------------------------------------ softmax
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegsSoftmax));
+    const int i = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t t_row = tmem + i * kTmemCols + ((uint32_t)((warp & 3) * 32) << 16);
+    const float c = 1.4426950408889634f * 0.125f;        // log2(e) / sqrt(64)
+    float m = -INFINITY, l = 0.0f;
+    bool ok = true, seen = false;                        // seen: some row is live
+    for (int idx = 0; idx < 2 * n_tiles && ok && i < n_q; ++idx) {                // idx = 2 * tile + half
+      const int it = idx >> 1, hf = idx & 1, col0 = (t_begin + it) * kBN + hf * kHalf;
+      uint32_t mask[kHalf / 32];
+      bool whole = P.live == nullptr && col0 + kHalf <= len;
+      if (!whole) {
+        whole = true;
+#pragma unroll
+        for (int j = 0; j < kHalf / 32; ++j) {
+          const int r = col0 + 32 * j + lane;
+          mask[j] = __ballot_sync(0xFFFFFFFFu, r < len && (P.live == nullptr || P.live[(size_t)seq * P.cap + r] != 0));
+          whole = whole && mask[j] == 0xFFFFFFFFu;
+          seen = seen || mask[j] != 0u;
+        }
+      } else {
+        seen = true;
+      }
+      ok = __all_sync(0xFFFFFFFFu, mbar_wait(&B->s_full[i][hf], (uint32_t)it & 1u, B, P.status)) != 0;
+      if (!ok) break;
+      tc_fence_after();
+      uint32_t s[kHalf];
+      auto load_scores = [&]() {
+#pragma unroll
+        for (int j = 0; j < kHalf / 32; ++j) tmem_ld32(t_row + kColS + hf * kHalf + j * 32, s + j * 32);
+        tmem_wait_ld();
+        if (!whole) {
+#pragma unroll
+          for (int j = 0; j < kHalf; ++j)
+            if (!(mask[j >> 5] >> (j & 31) & 1u)) s[j] = 0xFF800000u;
+        }
+      };
+      // p = 2^(s c - reference) on pairs, packed to bf16 over the front of s[]; returns the row's sum of p and its largest raw score
+      auto exp_pass = [&](auto track, float& raw) -> float {
+        const float ref = m == -INFINITY ? 0.0f : m;
+        const float2 c2 = make_float2(c, c), nm2 = make_float2(-ref, -ref);
+        float2 acc[4];
+        float m4[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          acc[q] = make_float2(0.0f, 0.0f);
+          m4[q] = -INFINITY;
+        }
+#pragma unroll
+        for (int j = 0; j < kHalf; j += 2) {
+          const float s0 = __uint_as_float(s[j]), s1 = __uint_as_float(s[j + 1]);
+          if constexpr (decltype(track)::value) m4[(j >> 1) & 3] = max3(m4[(j >> 1) & 3], s0, s1);
+          const float2 x = fma2(make_float2(s0, s1), c2, nm2);
+          const float2 p = pair_on_fma_pipes(j >> 1) ? ex2_poly2<true>(x) : make_float2(ex2(x.x), ex2(x.y));
+          acc[(j >> 1) & 3] = add2(acc[(j >> 1) & 3], p);
+          s[j >> 1] = pack_bf16(p.x, p.y);
+        }
+        raw = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+        const float2 t = add2(add2(acc[0], acc[1]), add2(acc[2], acc[3]));
+        return t.x + t.y;
+      };
+      load_scores();
+      float add, raw;
+      if (idx == 0) {
+        // the first half fixes the reference: its maximum has to be known before any exponential
+        float m4[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          m4[q] = fmaxf(__uint_as_float(s[24 * q]), __uint_as_float(s[24 * q + 1]));
+#pragma unroll
+          for (int j = 2; j < 24; j += 2) m4[q] = max3(m4[q], __uint_as_float(s[24 * q + j]), __uint_as_float(s[24 * q + j + 1]));
+        }
+        static_assert(kHalf == 96, "four chains of 24");
+        m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * c;
+        add = exp_pass(std::false_type{}, raw);
+      } else {
+        add = exp_pass(std::true_type{}, raw);
+        const float mx = raw * c;
+        const bool grow = mx - m > kRescaleThreshold;    // (also from nothing live to something)
+        if (__any_sync(0xFFFFFFFFu, grow)) {
+          // O may still be accumulating the half before: the scores of the next half, issued behind it, tell; or the last one's own barrier
+          ok = idx + 1 < 2 * n_tiles ? mbar_wait(&B->s_full[i][hf ^ 1], (uint32_t)((idx + 1) >> 1) & 1u, B, P.status)
+                                     : mbar_wait(&B->pv_done[i], 0, B, P.status);
+          ok = __all_sync(0xFFFFFFFFu, ok) != 0;
+          if (!ok) break;
+          tc_fence_after();
+          const float a = grow ? ex2(m - mx) : 1.0f;
+          if (grow) {
+            m = mx;
+            l *= a;
+          }
+          uint32_t o[16];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            tmem_ld16(t_row + kColO + j * 16, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * a);
+            tmem_st16(t_row + kColO + j * 16, o);
+          }
+          load_scores();
+          add = exp_pass(std::false_type{}, raw);
+        }
+      }
+      l += add;
+      tmem_st32(t_row + kColS + hf * kHalf, s);
+      tmem_st16(t_row + kColS + hf * kHalf + 32, s + 32);
+      tmem_wait_st();
+      tc_fence_before();
+      mbar_arrive(&B->p_full[i][hf]);
+    }
+    if (i < n_q) {
+      float* o_row = sO + (i * kBM + row) * kManyPitch;
+      if (n_tiles > 0 && ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&B->o_full[i], 0, B, P.status)) != 0;
+      tc_fence_after();
+      uint32_t o[32];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (n_tiles > 0 && ok) {
+          tmem_ld32(t_row + kColO + j * 32, o);
+          tmem_wait_ld();
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          *reinterpret_cast<uint4*>(o_row + 32 * j + 4 * e) = n_tiles > 0 && ok ? make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]) : make_uint4(0u, 0u, 0u, 0u);
+      }
+      // live rows, but no score that is a number, or one that is infinite
+      if ((seen && m == -INFINITY) || m == INFINITY) l = __int_as_float(0x7FC00000);
+      sO[kManyRows * kManyPitch + i * kBM + row] = m;
+      sO[kManyRows * (kManyPitch + 1) + i * kBM + row] = seen ? l : 0.0f;
+    }
+    // ---- the cluster's parts in order, a share of the rows each
+    tc_fence_before();
+    sync_all();
+    const int valid = min(kManyRows, rows - row0);
+    for (int u = rank * 256 + threadIdx.x; u < valid * 16; u += S * 256) {
+      const int r = u >> 4, c4 = u & 15;
+      float mx = -INFINITY, sum = 0.0f;
+      for (int s = 0; s < S; ++s) mx = fmaxf(mx, cluster.map_shared_rank(sO, s)[kManyRows * kManyPitch + r]);
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int s = 0; s < S; ++s) {
+        const float* part = cluster.map_shared_rank(sO, s);
+        const float mi = part[kManyRows * kManyPitch + r], k = mi == mx ? 1.0f : exp2f(mi - mx);
+        const float4 x = *reinterpret_cast<const float4*>(part + r * kManyPitch + 4 * c4);
+        sum = fmaf(k, part[kManyRows * (kManyPitch + 1) + r], sum);
+        a.x = fmaf(k, x.x, a.x); a.y = fmaf(k, x.y, a.y); a.z = fmaf(k, x.z, a.z); a.w = fmaf(k, x.w, a.w);
+      }
+      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+      *reinterpret_cast<uint2*>(P.out + q_at(row0 + r) + 4 * c4) = make_uint2(pack_bf16(a.x * inv, a.y * inv), pack_bf16(a.z * inv, a.w * inv));
+    }
+    if (S > 1) sync_all();                               // (nobody leaves while its part is being read)
+  }
+}
+
+// CTAs that share the cached rows: waves over 148 SMs, each as long as its tiles of 192 rows and three more (set-up, joining).
+inline int many_parts(long long jobs, int cap) {
+  const int tiles = (cap + kBN - 1) / kBN;
+  int best = 1;
+  long long best_cost = -1;
+  for (int s = 1; s <= 8 && s <= tiles; ++s) {
+    const long long cost = (jobs * s + 147) / 148 * ((tiles + s - 1) / s + 3);
+    if (best_cost < 0 || cost < best_cost) best_cost = cost, best = s;
+  }
+  return best;
+}
+
+constexpr int kManyFrom = 65;          // rows from which that kernel is taken
+
 static inline int attn_q8_launch(AttnQ8Args P, cudaStream_t st) {
-  const int rows = P.M * P.group, tile = rows <= 8 ? 8 : (rows <= 16 ? 16 : 32);
+  const int rows = P.M * P.group;
+  if (rows >= kManyFrom) {
+    P.q_tiles = (rows + kManyRows - 1) / kManyRows;
+    const long long jobs = (long long)P.seqs * P.HK * P.q_tiles;
+    const int S = many_parts(jobs, P.cap);
+    if (jobs * S > 0x7FFFFFFF) return OVGGT_ERR_UNSUPPORTED;
+    static std::atomic<uint64_t> smem_many;
+    cudaError_t e = allow_smem(k_attn_q8_many, kManySmem, smem_many);
+    if (e == cudaSuccess) e = launch_dependent(k_attn_q8_many, dim3((unsigned)(jobs * S)), kManyThreads, S, kManySmem, st, true, P);
+    if (e != cudaSuccess) { g_attn_last_error = (int)e; return OVGGT_ERR_CUDA; }
+    return OVGGT_OK;
+  }
+  const int tile = rows <= 8 ? 8 : (rows <= 16 ? 16 : 32);
   P.q_tiles = (rows + tile - 1) / tile;
   const long long jobs = (long long)P.seqs * P.HK * P.q_tiles;
   // CTAs that share a head: as many as fill the SMs twice, while a warp has a tile to take
