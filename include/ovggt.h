@@ -403,11 +403,13 @@ int ovggt_k_load_q8(const int8_t* kq, const uint8_t* kx, const int8_t* vq, const
 /* out [n_seqs, M, n_heads * 64] = softmax(Q K^T / sqrt(64)) V over the rows of an 8-bit cache, bf16 queries and output: row j of sequence s
  * takes part if j < lens[s] (device [n_seqs], NULL = capacity; taken as 0 below 0 and as capacity above it) and live[s, j] != 0 (device
  * [n_seqs, capacity] uint8, NULL = all).  Where no row does, out is 0.  Query head h reads key head h / (n_heads / n_kv_heads); n_heads
- * a multiple of n_kv_heads.  Rows that do not take part are not looked at: they may hold anything.  device_status: device int, as for
- * ovggt_k_attention.  No scratch memory. */
+ * a multiple of n_kv_heads.  Rows that do not take part may hold anything.  scratch: device, >= ovggt_k_attention_q8_scratch_bytes
+ * (0 if the sizes are invalid); it need not hold anything, and calls that may overlap need one each.  device_status: device int, as for
+ * ovggt_k_attention. */
+size_t ovggt_k_attention_q8_scratch_bytes(int32_t n_seqs, int32_t M, int32_t n_heads, int32_t n_kv_heads, int32_t capacity);
 int ovggt_k_attention_q8(const void* q, const int8_t* kq, const uint8_t* kx, const int8_t* vq, const uint8_t* vx, int32_t n_seqs,
                          int32_t M, int32_t n_heads, int32_t n_kv_heads, int32_t capacity, const int32_t* lens, const uint8_t* live,
-                         void* out, int32_t* device_status, void* stream);
+                         void* out, void* scratch, int32_t* device_status, void* stream);
 
 #ifdef __cplusplus
 }

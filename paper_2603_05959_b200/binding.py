@@ -35,7 +35,7 @@ EXPORTED = [
     "ovggt_k_diversity", "ovggt_k_diversity_static", "ovggt_k_select", "ovggt_k_compact", "ovggt_k_attention_scratch_bytes",
     "ovggt_k_attention", "ovggt_k_key_norm_bound", "ovggt_k_attention_bounded", "ovggt_k_gemm_bf16",
     "ovggt_k_linear_bf16", "ovggt_k_norm_q8", "ovggt_k_linear_q8", "ovggt_k_store_q8", "ovggt_k_load_q8",
-    "ovggt_k_attention_q8",
+    "ovggt_k_attention_q8_scratch_bytes", "ovggt_k_attention_q8",
 ]
 
 
@@ -133,7 +133,9 @@ def lib():
         L.ovggt_k_linear_q8.argtypes = [vp, vp, vp, vp, i32, i32, i32, C.POINTER(vp), i32, i32, vp, vp, vp, vp]
         L.ovggt_k_store_q8.argtypes = [vp, vp, i32, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp]
         L.ovggt_k_load_q8.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp]
-        L.ovggt_k_attention_q8.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp]
+        L.ovggt_k_attention_q8_scratch_bytes.restype = C.c_size_t
+        L.ovggt_k_attention_q8_scratch_bytes.argtypes = [i32, i32, i32, i32, i32]
+        L.ovggt_k_attention_q8.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp]
         L.ovggt_k_attention_bounded.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp]
         assert _FRAME_IO.size == C.sizeof(OvggtFrameIO)
         for name in ("ovggt_layer_attend", "ovggt_layer_compress", "ovggt_layer_step", "ovggt_layer_step_host"):
@@ -620,7 +622,7 @@ def k_load_q8(cache, n: int, first: int = 0, dtype=torch.bfloat16, stream=None):
     return k, v
 
 
-def k_attention_q8(q: torch.Tensor, cache, lens=None, live=None, out=None, status=None, stream=None) -> torch.Tensor:
+def k_attention_q8(q: torch.Tensor, cache, lens=None, live=None, out=None, scratch=None, status=None, stream=None) -> torch.Tensor:
     """softmax(q k / 8) v of queries q [n_seqs, M, heads * 64] (bf16) over the cache's live rows (uint8 [n_seqs, capacity]; None: all)
     within lens (int32 [n_seqs]; None: the capacity); 0 where there is none."""
     n_seqs, capacity, H = _cache_q8(cache)
@@ -632,10 +634,15 @@ def k_attention_q8(q: torch.Tensor, cache, lens=None, live=None, out=None, statu
     own = status is None
     if own:
         status = torch.zeros(16, dtype=torch.int32, device=q.device)
-    _here(q, *cache, lens, live, out, status)
+    need = lib().ovggt_k_attention_q8_scratch_bytes(n_seqs, q.shape[1], q.shape[2] // 64, H, capacity)
+    if scratch is None:
+        scratch = torch.empty(need, dtype=torch.uint8, device=q.device)
+    assert scratch.numel() * scratch.element_size() >= need
+    _here(q, *cache, lens, live, out, scratch, status)
     kq, kx, vq, vx = cache
     _check(lib().ovggt_k_attention_q8(_dptr(q), _dptr(kq), _dptr(kx), _dptr(vq), _dptr(vx), n_seqs, q.shape[1], q.shape[2] // 64, H, capacity,
-                                      _dptr(lens), _dptr(live), _dptr(out), _dptr(status), _stream_ptr(stream)), "ovggt_k_attention_q8")
+                                      _dptr(lens), _dptr(live), _dptr(out), _dptr(scratch), _dptr(status), _stream_ptr(stream)),
+           "ovggt_k_attention_q8")
     if own:
         _check(int(status[0].item()), "ovggt_k_attention_q8 (device status)")
     return out

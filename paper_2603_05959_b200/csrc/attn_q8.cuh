@@ -2,8 +2,6 @@
 // where no row is live.  Query heads h of a key head's group read that head; `rows` below are (token, query head of the group).
 #pragma once
 
-#include <cooperative_groups.h>
-
 #include "gemm_q8.cuh"
 
 namespace ovggt {
@@ -14,10 +12,16 @@ struct AttnQ8Args {
   const uint8_t *kx, *vx;              // [seqs, HK, cap]
   const int* lens;                     // [seqs] or nullptr: cap
   const uint8_t* live;                 // [seqs, cap] or nullptr
-  __nv_bfloat16* out;
-  int seqs, M, H, HK, cap, group, q_tiles;
+  __nv_bfloat16* out;                  // [seqs, M, H, 64]      (parts == 1)
+  float* o_part;                       // un-normalised results of the parts of the cached rows: [parts, seqs * M, H * 64]
+  float2* ml_part;                     // (reference maximum in log2 units, row sum): [parts, seqs * M, H]
+  int seqs, M, H, HK, cap, group, q_tiles, parts;
   int* status;
 };
+
+// What stands for a part without live rows: a maximum below every other's, so that it weighs nothing beside a part that has some, and
+// a sum that makes the result zero where no part has.
+constexpr float kDeadMax = -1e30f, kDeadSum = 1.0f;
 
 __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -39,8 +43,8 @@ __device__ __forceinline__ uint32_t int8_to_bf16x2(uint32_t x) { return sub_bf16
 // ---------------------------------------------------------------- few rows: the cache streams through, once per 8, 16 or 32 rows
 //
 // Bound by the cache's bytes.  A warp takes tiles of 32 cached rows by itself, with three of them on their way in its own stages
-// (no barrier in the loop); a cluster of CTAs shares a sequence and head, and its parts are joined through distributed shared
-// memory: no scratch memory, no second launch.
+// (no barrier in the loop); the warps' results are joined through shared memory, those of the CTAs that share a sequence and head (parts) by
+// the bf16 attention's merge kernel.
 //   scores  by int8 MMAs on the cached bytes as they are.  A row of Q is taken as whole numbers of 15 bits, q = 2^(e - 13) (256 hi + lo), two int8
 //           operands: exact for elements down to 2^-6 of the row's largest, to 2^-14 of it for the rest.  With at
 //           most 8 rows hi and lo are the two halves of one operand of 16 rows.
@@ -51,21 +55,18 @@ __device__ __forceinline__ uint32_t int8_to_bf16x2(uint32_t x) { return sub_bf16
 constexpr int kFewWarps = 8, kFewStages = 3, kFewKeys = 32;
 constexpr int kFewX = 2 * kFewKeys * 64;                 // of a stage: K, V, then the exponents of K and V and the mask, 32 bytes each
 constexpr int kFewStage = kFewX + 128;
-__host__ __device__ constexpr int few_smem_bytes(int rows) { return kFewWarps * kFewStages * kFewStage + rows * (64 + 2) * 4; }
+__host__ __device__ constexpr int few_smem_bytes() { return kFewWarps * kFewStages * kFewStage; }
 static_assert(kFewStages * kFewStage >= 32 * (64 + 2) * 4, "a warp's result does not fit its stages");
 
 template <int ROWS>
 __global__ void __launch_bounds__(kFewWarps * 32) k_attn_q8_few(const AttnQ8Args P) {
-  namespace cg = cooperative_groups;
   constexpr bool PACK = ROWS == 8;
   constexpr int T = PACK ? 1 : ROWS / 16;                // operands of 16 rows
   constexpr int R = PACK ? 1 : 2;                        // rows of an operand a thread holds scores of
   extern __shared__ __align__(1024) unsigned char smem[];
-  cg::cluster_group cluster = cg::this_cluster();
-  const int S = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const long long job = blockIdx.x / S;
-  const int hk = (int)(job % P.HK), qt = (int)(job / P.HK % P.q_tiles), seq = (int)(job / P.HK / P.q_tiles);
+  const int hk = (int)(blockIdx.x % P.HK), qt = (int)(blockIdx.x / P.HK % P.q_tiles), rest = (int)(blockIdx.x / P.HK / P.q_tiles);
+  const int part = rest % P.parts, seq = rest / P.parts;
   const int rows = P.M * P.group, row0 = qt * ROWS;
   pdl_trigger();
   pdl_wait();
@@ -127,7 +128,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) k_attn_q8_few(const AttnQ8Args
   // ---- the cache, tile by tile
   unsigned char* stages = smem + warp * kFewStages * kFewStage;
   const size_t pitch = (size_t)P.HK * 64, base = ((size_t)seq * P.cap * P.HK + hk) * 64, xbase = ((size_t)seq * P.HK + hk) * P.cap;
-  const int first = rank * kFewWarps + warp, stride = S * kFewWarps;
+  const int first = part * kFewWarps + warp, stride = P.parts * kFewWarps;
   auto request = [&](int tile, int stage) {
     if (tile < tiles) {
       unsigned char* s = stages + stage * kFewStage;
@@ -301,12 +302,11 @@ __global__ void __launch_bounds__(kFewWarps * 32) k_attn_q8_few(const AttnQ8Args
         }
     }
   __syncthreads();
-  // ---- the CTA's, then the cluster's: out = sum O_i 2^(m_i - m) / sum l_i 2^(m_i - m) over the parts in order
-  auto weight = [](float mi, float mx) { return mi == mx ? 1.0f : exp2f(mi - mx); };   // (both -inf: nothing was live)
-  float* whole = reinterpret_cast<float*>(smem + kFewWarps * kFewStages * kFewStage);
+  // ---- the CTA's: sum O_i 2^(m_i - m), sum l_i 2^(m_i - m) over its warps in order
   constexpr int kPart = kFewStages * kFewStage / 4;
   for (int u = threadIdx.x; u < ROWS * 16; u += kFewWarps * 32) {
     const int row = u >> 4, c4 = u & 15;
+    if (row0 + row >= rows) break;
     const float* parts = reinterpret_cast<const float*>(smem);
     float mx = -INFINITY, sum = 0.0f;
 #pragma unroll
@@ -314,61 +314,31 @@ __global__ void __launch_bounds__(kFewWarps * 32) k_attn_q8_few(const AttnQ8Args
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int w = 0; w < kFewWarps; ++w) {
-      const float k = weight(parts[w * kPart + ROWS * 64 + row], mx);
+      const float mi = parts[w * kPart + ROWS * 64 + row], k = mi == mx ? 1.0f : exp2f(mi - mx);   // (both -inf: nothing was live)
       const float4 x = *reinterpret_cast<const float4*>(parts + w * kPart + row * 64 + 4 * c4);
       sum = fmaf(k, parts[w * kPart + ROWS * 65 + row], sum);
       a.x = fmaf(k, x.x, a.x); a.y = fmaf(k, x.y, a.y); a.z = fmaf(k, x.z, a.z); a.w = fmaf(k, x.w, a.w);
     }
-    *reinterpret_cast<float4*>(whole + row * 64 + 4 * c4) = a;
-    if (c4 == 0) whole[ROWS * 64 + row] = mx, whole[ROWS * 65 + row] = sum;
-  }
-  if (S > 1) cluster.sync(); else __syncthreads();
-  for (int u = rank * kFewWarps * 32 + threadIdx.x; u < ROWS * 16; u += S * kFewWarps * 32) {
-    const int row = u >> 4, c4 = u & 15;
-    if (row0 + row >= rows) continue;
-    float mx = -INFINITY, sum = 0.0f;
-    for (int s = 0; s < S; ++s) mx = fmaxf(mx, cluster.map_shared_rank(whole, s)[ROWS * 64 + row]);
-    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s = 0; s < S; ++s) {
-      const float* part = cluster.map_shared_rank(whole, s);
-      const float k = weight(part[ROWS * 64 + row], mx);
-      const float4 x = *reinterpret_cast<const float4*>(part + row * 64 + 4 * c4);
-      sum = fmaf(k, part[ROWS * 65 + row], sum);
-      a.x = fmaf(k, x.x, a.x); a.y = fmaf(k, x.y, a.y); a.z = fmaf(k, x.z, a.z); a.w = fmaf(k, x.w, a.w);
+    const size_t at = q_at(row0 + row);
+    if (P.parts == 1) {
+      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+      *reinterpret_cast<uint2*>(P.out + at + 4 * c4) = make_uint2(pack_bf16(a.x * inv, a.y * inv), pack_bf16(a.z * inv, a.w * inv));
+    } else {
+      const size_t to = (size_t)part * P.seqs * P.M * P.H * 64 + at;
+      *reinterpret_cast<float4*>(P.o_part + to + 4 * c4) = a;
+      if (c4 == 0) P.ml_part[to / 64] = make_float2(mx == -INFINITY ? kDeadMax : mx, sum == 0.0f ? kDeadSum : sum);
     }
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    *reinterpret_cast<uint2*>(P.out + q_at(row0 + row) + 4 * c4) = make_uint2(pack_bf16(a.x * inv, a.y * inv), pack_bf16(a.z * inv, a.w * inv));
   }
-  if (S > 1) cluster.sync();                             // (nobody leaves while its part is being read)
 }
 
-// ---------------------------------------------------------------- many rows: tcgen05, the cache widened on its way into shared memory
+// ---------------------------------------------------------------- many rows: tcgen05 over bf16 planes
 //
-// The bf16 attention's scheme (see attn_tcgen05.cuh: halves of 96 cached rows with a buffer of scores each, so that the MMAs of one half run
-// under the softmax of the other) for two tiles of 128 rows a CTA, whose K and V tiles six warps read as int8 and write as bf16 planes, once
-// for both: q 2^(x - 133) is exact in bf16, so the operands are what the cache stands for.  A plane costs 2.5 instructions an element,
-// shared by 256 rows; a pass of its own that writes bf16 planes to memory would move 5 bytes an element instead of one.
-//   warps 0-7    softmax, four a tile, one thread a row; the running maximum moves when it is outgrown by 2^8 and O is rescaled then
-//   warps 8, 9   MMA issuers, one a tile; warp 8 allocates tensor memory (2 x 256 columns)
-//   warps 10-15  K and V: copied to shared memory two tiles ahead, widened there
-// The cached rows of a sequence and head are shared out over a cluster of CTAs, whose parts are joined through distributed shared memory.
-// Every wait is bounded; on expiry the CTA records OVGGT_ERR_TIMEOUT and leaves through the common teardown.
-constexpr int kManyThreads = 512, kManyConverters = 192, kManyRows = 2 * kBM;
-constexpr int kManyRegsSoftmax = 200, kManyRegsOther = 56;
-static_assert(256 * kManyRegsSoftmax + 256 * kManyRegsOther <= kManyThreads * kRegsLaunch, "register pool of the CTA exceeded");
-constexpr int kManyPitch = kHD + 4;                      // floats between the rows of O in shared memory
-
-struct ManyBarriers {
-  unsigned long long k_full[kKVStages], k_empty[kKVStages], v_full[kKVStages], v_empty[kKVStages];
-  unsigned long long s_full[2][2], p_full[2][2], pv_done[2], o_full[2], drain[2];   // by row tile
-  uint32_t tmem_base;
-  int abort_flag;
-};
-constexpr int kManyRaw = 3, kManyRawStage = 2 * kBN * kHD;   // stages of K and V tiles as they lie in the cache; O, maxima and sums come to lie over them
-constexpr int kManyO = 2 * kQBytes + 2 * kKVStages * kTileBytes;
-constexpr int kManyBar = kManyO + kManyRaw * kManyRawStage;
-static_assert(kManyRows * (kManyPitch + 2) * 4 <= kManyRaw * kManyRawStage, "a CTA's result does not fit the tiles it lies over");
-constexpr int kManySmem = kManyBar + (int)sizeof(ManyBarriers);
+// From two tiles of queries or so on, widening the cache once, into bf16 planes in scratch memory, costs less than each tile's doing it: a
+// plane takes 2.5 instructions an element and 5 bytes of traffic, most of it in L2 (17758 rows of 16 heads: 18 us beside 120 of
+// attention for 11 tiles of queries; widened on the way into shared memory, once for two tiles, the same attention took 250 us: the
+// widening warps share the issue slots with the softmax).  The planes are what the cache stands for: q 2^(x - 133) is exact in bf16.
+constexpr size_t kPlanesAtOnce = (size_t)128 << 20;      // bytes of planes up to which sequences are taken together: what stays in L2
+constexpr size_t kPlanesMost = (size_t)2 << 30;          // beyond which the few-row kernel takes any number of rows
 
 // 2^(x - 133) as a pair of bf16; NaN for 255.
 __device__ __forceinline__ uint32_t q8_step_bf16x2(uint32_t x) { return (x == 255u ? 0x7FFFu : (max(x, 6u) - 6u) << 7) * 0x00010001u; }
@@ -376,81 +346,111 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   const __nv_bfloat162 d = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
   return *reinterpret_cast<const uint32_t*>(&d);
 }
-// 16 int8 of columns [16 c, 16 c + 16) of row r, times step -> the same place of a swizzled bf16 tile.
-__device__ __forceinline__ void store_widened(unsigned char* tile, int r, int c, const uint4& w, uint32_t step) {
-  const uint32_t in[4] = {w.x, w.y, w.z, w.w};
+
+struct WidenArgs {
+  const uint4 *kq, *vq;                // [seqs, cap, HK * 64] int8
+  const uint8_t *kx, *vx;
+  const int* lens;
+  const uint8_t* live;
+  uint4 *k, *v;                        // [seqs, rows, HK * 64] bf16
+  int seqs, cap, HK, rows;             // rows: the capacity up to whole tiles
+};
+
+// Sixteen elements a thread; rows past the length, up to the end of its last tile, become zeros, as do values that are masked.  A
+// value whose key is not finite becomes NaN with it: its weight makes the result NaN whatever it comes out as.
+__global__ void __launch_bounds__(256) k_widen_q8(const WidenArgs P) {
+  pdl_trigger();
+  pdl_wait();
+  const int seq = blockIdx.y, side = blockIdx.z;
+  const long long at = (long long)blockIdx.x * 256 + threadIdx.x, block = at >> 2;
+  const long long row = block / P.HK;
+  const int h = (int)(block - row * P.HK);
+  const int len = min(P.cap, max(0, P.lens != nullptr ? P.lens[seq] : P.cap));
+  if (row >= (len + kBN - 1) / kBN * kBN) return;
+  uint4 w = make_uint4(0u, 0u, 0u, 0u);
+  uint32_t x = 0u;
+  if (row < len) {
+    w = ld_nc((side == 0 ? P.kq : P.vq) + (((size_t)seq * P.cap + row) * P.HK + h) * 4 + (at & 3));
+    const size_t xat = ((size_t)seq * P.HK + h) * P.cap + row;
+    x = P.kx[xat];
+    if (side == 1) x = P.live != nullptr && P.live[(size_t)seq * P.cap + row] == 0 ? 0u : (x == 255u ? 255u : P.vx[xat]);
+  }
+  const uint32_t step = q8_step_bf16x2(x), in[4] = {w.x, w.y, w.z, w.w};
   uint32_t o[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     o[2 * i] = mul_bf16x2(int8_to_bf16x2(__byte_perm(in[i], 0x43434343u, 0x4140)), step);
     o[2 * i + 1] = mul_bf16x2(int8_to_bf16x2(__byte_perm(in[i], 0x43434343u, 0x4342)), step);
   }
-  unsigned char* p = tile + r * 128;
-  *reinterpret_cast<uint4*>(p + (((2 * c) ^ (r & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
-  *reinterpret_cast<uint4*>(p + (((2 * c + 1) ^ (r & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+  uint4* d = (side == 0 ? P.k : P.v) + (size_t)seq * P.rows * P.HK * 8 + 2 * (size_t)at;
+  d[0] = make_uint4(o[0], o[1], o[2], o[3]);
+  d[1] = make_uint4(o[4], o[5], o[6], o[7]);
 }
 
-__global__ void __launch_bounds__(kManyThreads, 1) k_attn_q8_many(const __grid_constant__ AttnQ8Args P) {
-  namespace cg = cooperative_groups;
+// The bf16 attention's scheme (see attn_tcgen05.cuh: the same warps, tiles, halves and order of MMAs, two CTAs an SM) with lengths and masks
+// that are read here, sequences and shared heads, and rows without a live cached row.
+constexpr int kManyBar = kQBytes + 2 * kKVStages * kTileBytes;
+constexpr int kManySmem = kManyBar + (int)sizeof(AttnBarriers) + 64;
+
+__global__ void __launch_bounds__(kAttnThreads, kCtasPerSm)
+k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ AttnQ8Args P, const int plane_rows) {
   extern __shared__ __align__(1024) unsigned char smem[];
-  cg::cluster_group cluster = cg::this_cluster();
-  const int S = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-  const bool aligned = (smem_u32(smem) & 1023u) == 0;    // the 128-byte swizzle needs 1024-byte aligned tiles
-  if (!aligned && threadIdx.x == 0) report_status(P.status, OVGGT_ERR_DEVICE_STATUS);
+  if (smem_u32(smem) & 1023u) {                          // the 128-byte swizzle needs 1024-byte aligned tiles
+    if (threadIdx.x == 0) report_status(P.status, OVGGT_ERR_DEVICE_STATUS);
+    return;
+  }
   unsigned char* sQ = smem;
-  unsigned char* sK = sQ + 2 * kQBytes;
+  unsigned char* sK = sQ + kQBytes;
   unsigned char* sV = sK + kKVStages * kTileBytes;
-  unsigned char* sRaw = smem + kManyO;
-  float* sO = reinterpret_cast<float*>(sRaw);            // [256][kManyPitch], then maxima [256], sums [256], once every tile has been widened
-  ManyBarriers* B = reinterpret_cast<ManyBarriers*>(smem + kManyBar);
+  AttnBarriers* B = reinterpret_cast<AttnBarriers*>(smem + kManyBar);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long job = blockIdx.x / S;
-  const int hk = (int)(job % P.HK), qt = (int)(job / P.HK % P.q_tiles), seq = (int)(job / P.HK / P.q_tiles);
-  const int rows = P.M * P.group, row0 = qt * kManyRows, n_q = min(2, (rows - row0 + kBM - 1) / kBM);   // row tiles of this CTA
+  const int qt = (int)(blockIdx.x % P.q_tiles), hk = (int)(blockIdx.x / P.q_tiles % P.HK), rest = (int)(blockIdx.x / P.q_tiles / P.HK);
+  const int part = rest % P.parts, seq = rest / P.parts;
+  const int rows = P.M * P.group, row0 = qt * kBM;
   auto q_at = [&](int r) {                               // (row r is token r / group, head r % group of this group)
     const int m = r / P.group;
     return (((size_t)seq * P.M + m) * P.H + (size_t)hk * P.group + (r - m * P.group)) * kHD;
   };
   pdl_trigger();
-
-  if (threadIdx.x == 0) {
-    for (int s = 0; s < kKVStages; ++s) {
-      mbar_init(&B->k_full[s], kManyConverters);
-      mbar_init(&B->v_full[s], kManyConverters);
-      mbar_init(&B->k_empty[s], n_q);
-      mbar_init(&B->v_empty[s], n_q);
+  if (warp == 4 && lane == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_k) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_v) : "memory");
+    for (int hf = 0; hf < 2; ++hf) {
+      mbar_init(&B->s_full[hf], 1);
+      mbar_init(&B->p_full[hf], 128);
     }
-    for (int i = 0; i < 2; ++i) {
-      for (int hf = 0; hf < 2; ++hf) {
-        mbar_init(&B->s_full[i][hf], 1);
-        mbar_init(&B->p_full[i][hf], 128);
-      }
-      mbar_init(&B->pv_done[i], 1);
-      mbar_init(&B->o_full[i], 1);
-      mbar_init(&B->drain[i], 1);
+    mbar_init(&B->pv_done, 1);
+    mbar_init(&B->o_full, 1);
+    mbar_init(&B->drain, 1);
+    for (int s = 0; s < kKVStages; ++s) {
+      mbar_init(&B->k_full[s], 1);
+      mbar_init(&B->k_empty[s], 1);
+      mbar_init(&B->v_empty[s], 1);
+      mbar_init(&B->v_full[s], 1);
     }
     B->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  if (warp == 8) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&B->tmem_base)), "r"((uint32_t)(2 * kTmemCols)) : "memory");
+  if (warp == 5) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&B->tmem_base)), "r"((uint32_t)kTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   pdl_wait();
   const int len = min(P.cap, max(0, P.lens != nullptr ? P.lens[seq] : P.cap));
   const int tiles_total = (len + kBN - 1) / kBN;
-  const int t_begin = (int)((long long)rank * tiles_total / S), n_tiles = aligned ? (int)((long long)(rank + 1) * tiles_total / S) - t_begin : 0;
-  {                                                      // Q: 256 rows x 8 groups of 8 columns, rows past the last zero
-    constexpr int kPer = kManyRows * 8 / kManyThreads;
+  const int t_begin = (int)((long long)part * tiles_total / P.parts), n_tiles = (int)((long long)(part + 1) * tiles_total / P.parts) - t_begin;
+  {                                                      // Q: 128 rows x 8 groups of 8 columns, rows past the last zero
+    constexpr int kPer = kBM * 8 / kAttnThreads;
     uint4 x[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int idx = threadIdx.x + i * kManyThreads, r = row0 + (idx >> 3);
+      const int idx = threadIdx.x + i * kAttnThreads, r = row0 + (idx >> 3);
       x[i] = r < rows ? *reinterpret_cast<const uint4*>(P.q + q_at(r) + (idx & 7) * 8) : make_uint4(0u, 0u, 0u, 0u);
     }
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int idx = threadIdx.x + i * kManyThreads, r = idx >> 3;
+      const int idx = threadIdx.x + i * kAttnThreads, r = idx >> 3;
       *reinterpret_cast<uint4*>(sQ + r * 128 + (((idx & 7) ^ (r & 7)) << 4)) = x[i];
     }
   }
@@ -459,158 +459,107 @@ __global__ void __launch_bounds__(kManyThreads, 1) k_attn_q8_many(const __grid_c
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *(volatile uint32_t*)&B->tmem_base;
-  // Every warp of the cluster meets here at the end, each in its own branch: what follows a change of registers stays in it.
-  auto sync_all = [&]() {
-    __syncwarp();
-    if (S > 1) cluster.sync(); else asm volatile("barrier.sync.aligned 0;" ::: "memory");
-  };
 
-  if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kManyRegsOther));
-    if (warp < 10) {
-      // ------------------------------------------------ MMA issuers, in the bf16 attention's order:
+  if (warp >= 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
+    if (warp == 4) {
+      // ------------------------------------------------ TMA producer
+      if (lane == 0) {
+        int issued_k = 0, issued_v = 0;
+        bool ok = true;
+        for (int it = 0; it < n_tiles && ok; ++it) {
+          const int s = it % kKVStages, row = seq * plane_rows + (t_begin + it) * kBN;
+          const uint32_t ph = (uint32_t)(it / kKVStages - 1) & 1u;
+          if (it >= kKVStages) ok = mbar_wait(&B->k_empty[s], ph, B, P.status);
+          if (!ok) break;
+          mbar_expect_tx(&B->k_full[s], kTileBytes);
+          tma_load_2d(sK + s * kTileBytes, &tm_k, hk * kHD, row, &B->k_full[s]);
+          ++issued_k;
+          if (it >= kKVStages) ok = mbar_wait(&B->v_empty[s], ph, B, P.status);
+          if (!ok) break;
+          mbar_expect_tx(&B->v_full[s], kTileBytes);
+          tma_load_2d(sV + s * kTileBytes, &tm_v, hk * kHD, row, &B->v_full[s]);
+          ++issued_v;
+        }
+        if (!ok) {
+          // leave no bulk copy in flight into this CTA's shared memory
+          for (int i = max(0, issued_k - kKVStages); i < issued_k; ++i)
+            mbar_wait(&B->k_full[i % kKVStages], (uint32_t)(i / kKVStages) & 1u, B, P.status);
+          for (int i = max(0, issued_v - kKVStages); i < issued_v; ++i)
+            mbar_wait(&B->v_full[i % kKVStages], (uint32_t)(i / kKVStages) & 1u, B, P.status);
+        }
+      }
+      __syncwarp();
+    } else if (warp == 5 && n_tiles > 0) {
+      // ------------------------------------------------ MMA issuer, in the bf16 attention's order:
       // QK(0,0) QK(0,1) | PV(0,0) QK(1,0) PV(0,1) QK(1,1) | PV(1,0) QK(2,0) ...
-      const int i = warp - 8;
-      if (i < n_q && n_tiles > 0) {
-        const bool leader = elect_one();
-        const uint32_t tm = __reduce_or_sync(0xFFFFFFFFu, tmem) + i * kTmemCols;
-        constexpr uint32_t idesc_qk = idesc_bf16(kHalf, false), idesc_pv = idesc_bf16(kHD, true);
-        const uint64_t dq = smem_desc_sw128(smem_u32(sQ + i * kQBytes));
-        auto wait_all = [&](void* bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, B, P.status)) != 0; };
-        auto issue_qk = [&](int st, int hf) {
-          const uint64_t dk = smem_desc_sw128(smem_u32(sK + st * kTileBytes + hf * (kTileBytes / 2)));
+      const bool leader = elect_one();
+      const uint32_t tm = __reduce_or_sync(0xFFFFFFFFu, tmem);
+      constexpr uint32_t idesc_qk = idesc_bf16(kHalf, false), idesc_pv = idesc_bf16(kHD, true);
+      const uint64_t dq = smem_desc_sw128(smem_u32(sQ));
+      auto wait_all = [&](void* bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, B, P.status)) != 0; };
+      auto issue_qk = [&](int st, int hf) {
+        const uint64_t dk = smem_desc_sw128(smem_u32(sK + st * kTileBytes + hf * (kTileBytes / 2)));
+        if (leader) {
+#pragma unroll
+          for (int kk = 0; kk < kHD / 16; ++kk) mma_ss(tm + kColS + hf * kHalf, dq + (uint64_t)(kk * 2), dk + (uint64_t)(kk * 2), idesc_qk, kk > 0);
+          tc_commit(&B->s_full[hf]);
+          if (hf == 1) tc_commit(&B->k_empty[st]);
+        }
+      };
+      bool ok = wait_all(&B->k_full[0], 0);
+      if (ok) {
+        tc_fence_after();
+        issue_qk(0, 0);
+        issue_qk(0, 1);
+      }
+      for (int it = 0; it < n_tiles && ok; ++it) {
+        const int s = it % kKVStages, s1 = (it + 1) % kKVStages;
+        const uint32_t ph = (uint32_t)(it / kKVStages) & 1u, ph1 = (uint32_t)((it + 1) / kKVStages) & 1u;
+        const bool more = it + 1 < n_tiles;
+        ok = wait_all(&B->v_full[s], ph);
+        if (!ok) break;
+        const uint64_t dv = smem_desc_sw128(smem_u32(sV + s * kTileBytes));
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          ok = wait_all(&B->p_full[hf], (uint32_t)it & 1u);
+          if (!ok) break;
+          tc_fence_after();
           if (leader) {
 #pragma unroll
-            for (int kk = 0; kk < kHD / 16; ++kk) mma_ss(tm + kColS + hf * kHalf, dq + (uint64_t)(kk * 2), dk + (uint64_t)(kk * 2), idesc_qk, kk > 0);
-            tc_commit(&B->s_full[i][hf]);
-            if (hf == 1) tc_commit(&B->k_empty[st]);
+            for (int kk = 0; kk < kHalf / 16; ++kk)
+              mma_ts(tm + kColO, tm + kColS + hf * kHalf + kk * 8, dv + (uint64_t)((hf * (kHalf / 16) + kk) * 128), idesc_pv, (it > 0 || hf > 0 || kk > 0));
+            if (hf == 1) tc_commit(&B->v_empty[s]);
+            if (!more && hf == 0) tc_commit(&B->pv_done);    // (the last half has no later score MMA to tell it by)
           }
-        };
-        bool ok = wait_all(&B->k_full[0], 0);
-        if (ok) {
-          tc_fence_after();
-          issue_qk(0, 0);
-          issue_qk(0, 1);
-        }
-        for (int it = 0; it < n_tiles && ok; ++it) {
-          const int s = it % kKVStages, s1 = (it + 1) % kKVStages;
-          const uint32_t ph = (uint32_t)(it / kKVStages) & 1u, ph1 = (uint32_t)((it + 1) / kKVStages) & 1u;
-          const bool more = it + 1 < n_tiles;
-          ok = wait_all(&B->v_full[s], ph);
-          if (!ok) break;
-          const uint64_t dv = smem_desc_sw128(smem_u32(sV + s * kTileBytes));
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            ok = wait_all(&B->p_full[i][hf], (uint32_t)it & 1u);
-            if (!ok) break;
-            tc_fence_after();
-            if (leader) {
-#pragma unroll
-              for (int kk = 0; kk < kHalf / 16; ++kk)
-                mma_ts(tm + kColO, tm + kColS + hf * kHalf + kk * 8, dv + (uint64_t)((hf * (kHalf / 16) + kk) * 128), idesc_pv, (it > 0 || hf > 0 || kk > 0));
-              if (hf == 1) tc_commit(&B->v_empty[s]);
-              if (!more && hf == 0) tc_commit(&B->pv_done[i]);   // (the last half has no later score MMA to tell it by)
+          if (more) {
+            if (hf == 0) {
+              ok = wait_all(&B->k_full[s1], ph1);
+              if (!ok) break;
+              tc_fence_after();
             }
-            if (more) {
-              if (hf == 0) {
-                ok = wait_all(&B->k_full[s1], ph1);
-                if (!ok) break;
-                tc_fence_after();
-              }
-              issue_qk(s1, hf);
-            }
+            issue_qk(s1, hf);
           }
-        }
-        if (ok) {
-          if (leader) tc_commit(&B->o_full[i]);
-          wait_all(&B->o_full[i], 0);
-        } else {
-          if (leader) tc_commit(&B->drain[i]);           // let every issued MMA finish before TMEM is freed
-          wait_all(&B->drain[i], 0);
         }
       }
-      __syncwarp();
-    } else if (n_tiles > 0) {
-      // ------------------------------------------------ K and V
-      // A thread has four adjacent rows of a tile, 16 columns of each, and reads back what it copied itself: no barrier between the copy
-      // and the widening.  (Two threads next to each other take their rows in another order: their stores go to different banks.)
-      const int ct = (int)threadIdx.x - 320, c = ct & 3, g = ct >> 2;
-      const size_t pitch = (size_t)P.HK * kHD, base = ((size_t)seq * P.cap * P.HK + hk) * kHD + c * 16, xbase = ((size_t)seq * P.HK + hk) * P.cap;
-      auto request = [&](int t) {
-        if (t < n_tiles) {
-          unsigned char* raw = sRaw + (t % kManyRaw) * kManyRawStage + ct * 16;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = (t_begin + t) * kBN + 4 * g + (i ^ (g & 1));
-            const size_t at = base + (size_t)min(r, len - 1) * pitch;
-            copy16(raw + i * (kManyConverters * 16), P.kq + at, r < len);
-            copy16(raw + (4 + i) * (kManyConverters * 16), P.vq + at, r < len);
-          }
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-      };
-      struct Bytes { uint32_t k, v, live; };               // of the four rows
-      auto bytes_of = [&](int t) {
-        const int r = (t_begin + t) * kBN + 4 * g;         // (the capacity is a multiple of 16)
-        Bytes b = {0u, 0u, 0xFFFFFFFFu};
-        if (t < n_tiles && r < len) {
-          b.k = __ldg(reinterpret_cast<const uint32_t*>(P.kx + xbase + r));
-          b.v = __ldg(reinterpret_cast<const uint32_t*>(P.vx + xbase + r));
-          if (P.live != nullptr) b.live = __ldg(reinterpret_cast<const uint32_t*>(P.live + (size_t)seq * P.cap + r));
-        }
-        return b;
-      };
-      auto widen = [&](bool values, int t, const Bytes& b, unsigned char* tiles) {
-        const unsigned char* raw = sRaw + (t % kManyRaw) * kManyRawStage + (values ? 4 : 0) * (kManyConverters * 16) + ct * 16;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int e = i ^ (g & 1), r = 4 * g + e;
-          uint32_t x = b.k >> (8 * e) & 255u;
-          // a row that is masked counts for nothing; one whose key is not finite makes the result NaN whatever its weight came out as
-          if (values) x = (b.live >> (8 * e) & 255u) == 0u ? 0u : (x == 255u ? 255u : b.v >> (8 * e) & 255u);
-          if ((t_begin + t) * kBN + r >= len) x = 0u;
-          store_widened(tiles + t % kKVStages * kTileBytes, r, c, *reinterpret_cast<const uint4*>(raw + i * (kManyConverters * 16)), q8_step_bf16x2(x));
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      };
-#pragma unroll
-      for (int t = 0; t < kManyRaw - 1; ++t) request(t);
-      Bytes next = bytes_of(0);
-#pragma unroll 1
-      for (int t = 0; t < n_tiles; ++t) {
-        const Bytes b = next;
-        next = bytes_of(t + 1);
-        request(t + kManyRaw - 1);
-        asm volatile("cp.async.wait_group %0;" ::"n"(kManyRaw - 1) : "memory");
-        const int s = t % kKVStages;
-        const uint32_t ph = (uint32_t)(t / kKVStages - 1) & 1u;
-        if (t >= kKVStages && !mbar_wait(&B->k_empty[s], ph, B, P.status)) break;
-        widen(false, t, b, sK);
-        mbar_arrive(&B->k_full[s]);
-        if (t >= kKVStages && !mbar_wait(&B->v_empty[s], ph, B, P.status)) break;
-        widen(true, t, b, sV);
-        mbar_arrive(&B->v_full[s]);
+      if (ok) {
+        if (leader) tc_commit(&B->o_full);
+        wait_all(&B->o_full, 0);
+      } else {
+        if (leader) tc_commit(&B->drain);                // let every issued MMA finish before TMEM is freed
+        wait_all(&B->drain, 0);
       }
-      asm volatile("cp.async.wait_group 0;" ::: "memory");
       __syncwarp();
     }
-    // ---- teardown: the softmax warps join the parts
-    tc_fence_before();
-    sync_all();
-    if (warp == 8) {
-      tc_fence_after();
-      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)(2 * kTmemCols)) : "memory");
-    }
-    if (S > 1) sync_all();
   } else {
-    // ------------------------------------------------ softmax
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegsSoftmax));
-    const int i = warp >> 2, row = (warp & 3) * 32 + lane;
-    const uint32_t t_row = tmem + i * kTmemCols + ((uint32_t)((warp & 3) * 32) << 16);
+    // ------------------------------------------------ softmax and epilogue, one thread a row
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+    const int row = warp * 32 + lane;
+    const uint32_t t_row = tmem + ((uint32_t)(warp * 32) << 16);
     const float c = 1.4426950408889634f * 0.125f;        // log2(e) / sqrt(64)
     float m = -INFINITY, l = 0.0f;
-    bool ok = true, seen = false;                        // seen: some row is live
-    for (int idx = 0; idx < 2 * n_tiles && ok && i < n_q; ++idx) {                // idx = 2 * tile + half
+    bool ok = true, seen = false;                        // seen: some cached row is live
+    for (int idx = 0; idx < 2 * n_tiles && ok; ++idx) {  // idx = 2 * tile + half
       const int it = idx >> 1, hf = idx & 1, col0 = (t_begin + it) * kBN + hf * kHalf;
       uint32_t mask[kHalf / 32];
       bool whole = P.live == nullptr && col0 + kHalf <= len;
@@ -626,7 +575,8 @@ __global__ void __launch_bounds__(kManyThreads, 1) k_attn_q8_many(const __grid_c
       } else {
         seen = true;
       }
-      ok = __all_sync(0xFFFFFFFFu, mbar_wait(&B->s_full[i][hf], (uint32_t)it & 1u, B, P.status)) != 0;
+      // (every wait result is made warp-uniform before the warp meets an .aligned tensor-memory instruction)
+      ok = __all_sync(0xFFFFFFFFu, mbar_wait(&B->s_full[hf], (uint32_t)it & 1u, B, P.status)) != 0;
       if (!ok) break;
       tc_fence_after();
       uint32_t s[kHalf];
@@ -669,13 +619,13 @@ __global__ void __launch_bounds__(kManyThreads, 1) k_attn_q8_many(const __grid_c
       if (idx == 0) {
         // the first half fixes the reference: its maximum has to be known before any exponential
         float m4[4];
+        constexpr int kChain = kHalf / 4;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          m4[q] = fmaxf(__uint_as_float(s[24 * q]), __uint_as_float(s[24 * q + 1]));
+          m4[q] = fmaxf(__uint_as_float(s[kChain * q]), __uint_as_float(s[kChain * q + 1]));
 #pragma unroll
-          for (int j = 2; j < 24; j += 2) m4[q] = max3(m4[q], __uint_as_float(s[24 * q + j]), __uint_as_float(s[24 * q + j + 1]));
+          for (int j = 2; j < kChain; j += 2) m4[q] = max3(m4[q], __uint_as_float(s[kChain * q + j]), __uint_as_float(s[kChain * q + j + 1]));
         }
-        static_assert(kHalf == 96, "four chains of 24");
         m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * c;
         add = exp_pass(std::false_type{}, raw);
       } else {
@@ -684,8 +634,8 @@ __global__ void __launch_bounds__(kManyThreads, 1) k_attn_q8_many(const __grid_c
         const bool grow = mx - m > kRescaleThreshold;    // (also from nothing live to something)
         if (__any_sync(0xFFFFFFFFu, grow)) {
           // O may still be accumulating the half before: the scores of the next half, issued behind it, tell; or the last one's own barrier
-          ok = idx + 1 < 2 * n_tiles ? mbar_wait(&B->s_full[i][hf ^ 1], (uint32_t)((idx + 1) >> 1) & 1u, B, P.status)
-                                     : mbar_wait(&B->pv_done[i], 0, B, P.status);
+          ok = idx + 1 < 2 * n_tiles ? mbar_wait(&B->s_full[hf ^ 1], (uint32_t)((idx + 1) >> 1) & 1u, B, P.status)
+                                     : mbar_wait(&B->pv_done, 0, B, P.status);
           ok = __all_sync(0xFFFFFFFFu, ok) != 0;
           if (!ok) break;
           tc_fence_after();
@@ -712,90 +662,155 @@ __global__ void __launch_bounds__(kManyThreads, 1) k_attn_q8_many(const __grid_c
       tmem_st16(t_row + kColS + hf * kHalf + 32, s + 32);
       tmem_wait_st();
       tc_fence_before();
-      mbar_arrive(&B->p_full[i][hf]);
+      mbar_arrive(&B->p_full[hf]);
     }
-    if (i < n_q) {
-      float* o_row = sO + (i * kBM + row) * kManyPitch;
-      if (n_tiles > 0 && ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&B->o_full[i], 0, B, P.status)) != 0;
+    if (n_tiles > 0 && ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&B->o_full, 0, B, P.status)) != 0;
+    if (ok) {
       tc_fence_after();
-      uint32_t o[32];
+      // Live rows, but no score that is a number, or one that is infinite: not a number.
+      if ((seen && m == -INFINITY) || m == INFINITY) l = __int_as_float(0x7FC00000);
+      const bool one = P.parts == 1;
+      const float inv = !seen ? 0.0f : (one ? 1.0f / l : 1.0f);
+      // By way of the operand tiles, which are free now: a thread has a row, but a warp stores whole lines of it.
+      unsigned char* stage = sK + warp * 32 * kOutRow;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        if (n_tiles > 0 && ok) {
+        uint32_t o[32];
+        if (n_tiles > 0) {
           tmem_ld32(t_row + kColO + j * 32, o);
           tmem_wait_ld();
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          *reinterpret_cast<uint4*>(o_row + 32 * j + 4 * e) = n_tiles > 0 && ok ? make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]) : make_uint4(0u, 0u, 0u, 0u);
+        for (int e = 0; e < 32; ++e) o[e] = seen ? __float_as_uint(__uint_as_float(o[e]) * inv) : 0u;
+        uint4* dst = reinterpret_cast<uint4*>(stage + lane * kOutRow);
+        if (one) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float* f = reinterpret_cast<const float*>(o) + 8 * e;
+            dst[4 * j + e] = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) dst[8 * j + e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+        }
       }
-      // live rows, but no score that is a number, or one that is infinite
-      if ((seen && m == -INFINITY) || m == INFINITY) l = __int_as_float(0x7FC00000);
-      sO[kManyRows * kManyPitch + i * kBM + row] = m;
-      sO[kManyRows * (kManyPitch + 1) + i * kBM + row] = seen ? l : 0.0f;
-    }
-    // ---- the cluster's parts in order, a share of the rows each
-    tc_fence_before();
-    sync_all();
-    const int valid = min(kManyRows, rows - row0);
-    for (int u = rank * 256 + threadIdx.x; u < valid * 16; u += S * 256) {
-      const int r = u >> 4, c4 = u & 15;
-      float mx = -INFINITY, sum = 0.0f;
-      for (int s = 0; s < S; ++s) mx = fmaxf(mx, cluster.map_shared_rank(sO, s)[kManyRows * kManyPitch + r]);
-      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int s = 0; s < S; ++s) {
-        const float* part = cluster.map_shared_rank(sO, s);
-        const float mi = part[kManyRows * kManyPitch + r], k = mi == mx ? 1.0f : exp2f(mi - mx);
-        const float4 x = *reinterpret_cast<const float4*>(part + r * kManyPitch + 4 * c4);
-        sum = fmaf(k, part[kManyRows * (kManyPitch + 1) + r], sum);
-        a.x = fmaf(k, x.x, a.x); a.y = fmaf(k, x.y, a.y); a.z = fmaf(k, x.z, a.z); a.w = fmaf(k, x.w, a.w);
+      __syncwarp();
+      const size_t shift = (size_t)part * P.seqs * P.M * P.H * kHD;
+      const int words = one ? 8 : 16;                    // 16-byte words of a row
+#pragma unroll 4
+      for (int u = lane; u < 32 * words; u += 32) {
+        const int r = u / words, w = u - r * words, at_row = row0 + warp * 32 + r;
+        if (at_row < rows) {
+          const uint4 x = *reinterpret_cast<const uint4*>(stage + r * kOutRow + w * 16);
+          if (one) *reinterpret_cast<uint4*>(P.out + q_at(at_row) + w * 8) = x;
+          else *reinterpret_cast<uint4*>(P.o_part + shift + q_at(at_row) + w * 4) = x;
+        }
       }
-      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-      *reinterpret_cast<uint2*>(P.out + q_at(row0 + r) + 4 * c4) = make_uint2(pack_bf16(a.x * inv, a.y * inv), pack_bf16(a.z * inv, a.w * inv));
+      if (!one && row0 + row < rows) P.ml_part[(shift + q_at(row0 + row)) / kHD] = make_float2(seen && m != -INFINITY ? m : kDeadMax, seen ? l : kDeadSum);
     }
-    if (S > 1) sync_all();                               // (nobody leaves while its part is being read)
+  }
+
+  // ------------------------------------------------ teardown
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 5) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)kTmemCols) : "memory");
   }
 }
 
-// CTAs that share the cached rows: waves over 148 SMs, each as long as its tiles of 192 rows and three more (set-up, joining).
-inline int many_parts(long long jobs, int cap) {
-  const int tiles = (cap + kBN - 1) / kBN;
-  int best = 1;
-  long long best_cost = -1;
-  for (int s = 1; s <= 8 && s <= tiles; ++s) {
-    const long long cost = (jobs * s + 147) / 148 * ((tiles + s - 1) / s + 3);
-    if (best_cost < 0 || cost < best_cost) best_cost = cost, best = s;
+// ---------------------------------------------------------------- host side
+
+constexpr int kManyFrom = 65;          // rows from which the planes are taken
+
+// How a call is cut: rows a CTA takes (8, 16, 32: the few-row kernel; 128), parts of the cached rows, sequences at once.
+struct AttnQ8Plan {
+  int tile, q_tiles, parts, seqs, plane_rows;
+  size_t planes, o_part, bytes;        // of scratch: K and V planes, the parts' results, all
+};
+inline AttnQ8Plan attn_q8_plan(int seqs, int M, int H, int HK, int cap) {
+  AttnQ8Plan A = {};
+  const long long rows = (long long)M * (H / HK);
+  A.plane_rows = (cap + kBN - 1) / kBN * kBN;
+  const size_t one = (size_t)A.plane_rows * HK * kHD * 4;
+  if (rows >= kManyFrom && one <= kPlanesMost) {
+    A.tile = kBM;
+    A.seqs = (int)std::max<size_t>(1, std::min<size_t>(seqs, kPlanesAtOnce / one));
+    A.planes = one * A.seqs;
+    A.q_tiles = (int)((rows + kBM - 1) / kBM);
+    // waves of CTAs over 2 x 148 places, each as long as its tiles and two more (set-up, epilogue), a merge one tile more
+    const int tiles = A.plane_rows / kBN;
+    const long long jobs = (long long)A.seqs * HK * A.q_tiles;
+    long long best = -1;
+    for (int s = 1; s <= kMaxSplits && s <= tiles; ++s) {
+      const long long cost = (jobs * s + 295) / 296 * ((tiles + s - 1) / s + 2) + (s > 1 ? 1 : 0);
+      if (best < 0 || cost < best) best = cost, A.parts = s;
+    }
+  } else {
+    A.tile = rows <= 8 ? 8 : (rows <= 16 ? 16 : 32);
+    A.seqs = seqs;
+    A.q_tiles = (int)((rows + A.tile - 1) / A.tile);
+    // as many CTAs as fit at once, while each warp has two tiles to take
+    const long long jobs = (long long)seqs * HK * A.q_tiles, places = 2 * 148, most = cap / (2 * kFewWarps * kFewKeys);
+    A.parts = (int)std::max(1ll, std::min({(long long)kMaxSplits, places / jobs, most}));
   }
-  return best;
+  A.o_part = A.parts == 1 ? 0 : (size_t)A.parts * A.seqs * M * H * kHD * 4;
+  A.bytes = A.planes + A.o_part + (A.parts == 1 ? 0 : (size_t)A.parts * A.seqs * M * H * 8);
+  return A;
 }
 
-constexpr int kManyFrom = 65;          // rows from which that kernel is taken
-
-static inline int attn_q8_launch(AttnQ8Args P, cudaStream_t st) {
-  const int rows = P.M * P.group;
-  if (rows >= kManyFrom) {
-    P.q_tiles = (rows + kManyRows - 1) / kManyRows;
-    const long long jobs = (long long)P.seqs * P.HK * P.q_tiles;
-    const int S = many_parts(jobs, P.cap);
-    if (jobs * S > 0x7FFFFFFF) return OVGGT_ERR_UNSUPPORTED;
-    static std::atomic<uint64_t> smem_many;
-    cudaError_t e = allow_smem(k_attn_q8_many, kManySmem, smem_many);
-    if (e == cudaSuccess) e = launch_dependent(k_attn_q8_many, dim3((unsigned)(jobs * S)), kManyThreads, S, kManySmem, st, true, P);
+static inline int attn_q8_launch(AttnQ8Args P, void* scratch, cudaStream_t st, int* launches) {
+  const AttnQ8Plan A = attn_q8_plan(P.seqs, P.M, P.H, P.HK, P.cap);
+  const int all = P.seqs;
+  P.q_tiles = A.q_tiles;
+  P.parts = A.parts;
+  P.o_part = reinterpret_cast<float*>(static_cast<char*>(scratch) + A.planes);
+  P.ml_part = reinterpret_cast<float2*>(static_cast<char*>(scratch) + A.planes + A.o_part);
+  const size_t q_seq = (size_t)P.M * P.H * kHD, rows_seq = (size_t)P.cap * P.HK * kHD, x_seq = (size_t)P.HK * P.cap;
+  *launches = 0;
+  for (int s0 = 0; s0 < all; s0 += A.seqs) {
+    P.seqs = std::min(A.seqs, all - s0);
+    const long long ctas = (long long)P.seqs * P.HK * P.q_tiles * P.parts;
+    if (ctas > 0x7FFFFFFF) return OVGGT_ERR_UNSUPPORTED;
+    cudaError_t e;
+    if (A.tile == kBM) {
+      char* planes = static_cast<char*>(scratch);
+      const size_t side = A.planes / 2;
+      const WidenArgs W = {reinterpret_cast<const uint4*>(P.kq), reinterpret_cast<const uint4*>(P.vq), P.kx, P.vx, P.lens, P.live,
+                           reinterpret_cast<uint4*>(planes), reinterpret_cast<uint4*>(planes + side), P.seqs, P.cap, P.HK, A.plane_rows};
+      CUtensorMap tk, tv;
+      int rc = make_rows_map(&tk, planes, P.seqs * A.plane_rows, P.HK * kHD, kBN);
+      if (rc) return rc;
+      rc = make_rows_map(&tv, planes + side, P.seqs * A.plane_rows, P.HK * kHD, kBN);
+      if (rc) return rc;
+      const long long widen = ((long long)A.plane_rows * P.HK * 4 + 255) / 256;
+      e = launch_dependent(k_widen_q8, dim3((unsigned)widen, P.seqs, 2), 256, 1, 0, st, true, W);
+      static std::atomic<uint64_t> smem_many;
+      if (e == cudaSuccess) e = allow_smem(k_attn_q8_many, kManySmem, smem_many);
+      if (e == cudaSuccess) e = launch_dependent(k_attn_q8_many, dim3((unsigned)ctas), kAttnThreads, 1, kManySmem, st, true, tk, tv, P, A.plane_rows);
+      *launches += 2;
+    } else {
+      const auto kernel = A.tile == 8 ? k_attn_q8_few<8> : (A.tile == 16 ? k_attn_q8_few<16> : k_attn_q8_few<32>);
+      static std::atomic<uint64_t> smem_few[3];
+      e = allow_smem(kernel, few_smem_bytes(), smem_few[A.tile == 8 ? 0 : (A.tile == 16 ? 1 : 2)]);
+      if (e == cudaSuccess) e = launch_dependent(kernel, dim3((unsigned)ctas), kFewWarps * 32, 1, few_smem_bytes(), st, true, P);
+      *launches += 1;
+    }
     if (e != cudaSuccess) { g_attn_last_error = (int)e; return OVGGT_ERR_CUDA; }
-    return OVGGT_OK;
+    if (P.parts > 1) {
+      const int rc = attn_merge_launch<__nv_bfloat16>(P.o_part, P.ml_part, P.seqs * P.M, P.H, P.parts, P.out, nullptr, st);
+      if (rc) return rc;
+      *launches += 1;
+    }
+    P.q += A.seqs * q_seq;
+    P.out += A.seqs * q_seq;
+    P.kq += A.seqs * rows_seq;
+    P.vq += A.seqs * rows_seq;
+    P.kx += A.seqs * x_seq;
+    P.vx += A.seqs * x_seq;
+    if (P.lens) P.lens += A.seqs;
+    if (P.live) P.live += (size_t)A.seqs * P.cap;
   }
-  const int tile = rows <= 8 ? 8 : (rows <= 16 ? 16 : 32);
-  P.q_tiles = (rows + tile - 1) / tile;
-  const long long jobs = (long long)P.seqs * P.HK * P.q_tiles;
-  // CTAs that share a head: as many as fill the SMs twice, while a warp has a tile to take
-  int S = 1;
-  while (S < 8 && jobs * S * 2 <= 2 * 148 && S * 2 * kFewWarps * kFewKeys <= P.cap) S *= 2;
-  if (jobs * S > 0x7FFFFFFF) return OVGGT_ERR_UNSUPPORTED;
-  const auto kernel = tile == 8 ? k_attn_q8_few<8> : (tile == 16 ? k_attn_q8_few<16> : k_attn_q8_few<32>);
-  static std::atomic<uint64_t> smem_set[3];
-  cudaError_t e = allow_smem(kernel, few_smem_bytes(tile), smem_set[tile == 8 ? 0 : (tile == 16 ? 1 : 2)]);
-  if (e == cudaSuccess) e = launch_dependent(kernel, dim3((unsigned)(jobs * S)), kFewWarps * 32, S, few_smem_bytes(tile), st, true, P);
-  if (e != cudaSuccess) { g_attn_last_error = (int)e; return OVGGT_ERR_CUDA; }
   return OVGGT_OK;
 }
 

@@ -1685,15 +1685,29 @@ extern "C" int ovggt_k_load_q8(const int8_t* kq, const uint8_t* kx, const int8_t
   return OVGGT_OK;
 }
 
+namespace {
+// (sizes whose products the kernels hold in 32 bits)
+bool attention_q8_fits(int32_t n_seqs, int32_t M, int32_t n_heads, int32_t capacity) {
+  return capacity % 16 == 0 && (long long)n_seqs * M * n_heads <= 0x7FFFFF00 && (long long)n_seqs * (capacity + 192ll) <= 0x7FFFFF00;
+}
+}  // namespace
+
+extern "C" size_t ovggt_k_attention_q8_scratch_bytes(int32_t n_seqs, int32_t M, int32_t n_heads, int32_t n_kv_heads, int32_t capacity) {
+  if (n_seqs < 1 || M < 1 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads != 0 || capacity < 1 ||
+      !attention_q8_fits(n_seqs, M, n_heads, capacity))
+    return 0;
+  return std::max<size_t>(16, attn_q8_plan(n_seqs, M, n_heads, n_kv_heads, capacity).bytes);
+}
+
 extern "C" int ovggt_k_attention_q8(const void* q, const int8_t* kq, const uint8_t* kx, const int8_t* vq, const uint8_t* vx, int32_t n_seqs,
                                     int32_t M, int32_t n_heads, int32_t n_kv_heads, int32_t capacity, const int32_t* lens,
-                                    const uint8_t* live, void* out, int32_t* device_status, void* stream) {
+                                    const uint8_t* live, void* out, void* scratch, int32_t* device_status, void* stream) {
   if (n_seqs == 0 || M == 0) return OVGGT_OK;
-  if (!q || !kq || !kx || !vq || !vx || !out || !device_status || n_seqs < 0 || M < 0 || n_heads < 1 || n_kv_heads < 1 || capacity < 1 ||
+  if (!q || !kq || !kx || !vq || !vx || !out || !scratch || !device_status || n_seqs < 0 || M < 0 || n_heads < 1 || n_kv_heads < 1 || capacity < 1 ||
       n_heads % n_kv_heads != 0)
     return OVGGT_ERR_INVALID_ARG;
-  if (capacity % 16 != 0 || (long long)M * n_heads > 0x7FFFFF00 || (long long)n_seqs * capacity > 0x7FFFFF00) return OVGGT_ERR_UNSUPPORTED;
-  if (!aligned16(q) || !aligned16(out) || !aligned16(kq) || !aligned16(vq) || !aligned16(kx) || !aligned16(vx) || !aligned16(live) ||
+  if (!attention_q8_fits(n_seqs, M, n_heads, capacity)) return OVGGT_ERR_UNSUPPORTED;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(scratch) || !aligned16(kq) || !aligned16(vq) || !aligned16(kx) || !aligned16(vx) || !aligned16(live) ||
       !aligned(lens, 4) || !aligned(device_status, 4))
     return OVGGT_ERR_MISALIGNED;
   AttnQ8Args P = {};
@@ -1703,8 +1717,9 @@ extern "C" int ovggt_k_attention_q8(const void* q, const int8_t* kq, const uint8
   P.out = static_cast<__nv_bfloat16*>(out);
   P.seqs = n_seqs; P.M = M; P.H = n_heads; P.HK = n_kv_heads; P.cap = capacity; P.group = n_heads / n_kv_heads;
   P.status = device_status;
-  const int rc = attn_q8_launch(P, static_cast<cudaStream_t>(stream));
-  if (rc == OVGGT_OK) g_launches.fetch_add(1);
+  int launches = 0;
+  const int rc = attn_q8_launch(P, scratch, static_cast<cudaStream_t>(stream), &launches);
+  g_launches.fetch_add(launches);
   if (rc == OVGGT_ERR_CUDA) cuda_fail((cudaError_t)attn_tcgen05_last_error());
   return rc;
 }

@@ -74,18 +74,27 @@ def test_store_and_load(lib):
     assert store(start=P + 2) == MISALIGNED
 
 
-ATTEND = dict(q=P, kq=P, kx=P, vq=P, vx=P, n_seqs=2, M=3, n_heads=8, n_kv_heads=4, capacity=32, lens=P, live=P, out=P, status=P, stream=None)
+ATTEND = dict(q=P, kq=P, kx=P, vq=P, vx=P, n_seqs=2, M=3, n_heads=8, n_kv_heads=4, capacity=32, lens=P, live=P, out=P, scratch=P, status=P, stream=None)
 
 
 def test_attention(lib):
     call = lambda **o: _call(lib.ovggt_k_attention_q8, list(ATTEND), ATTEND, **o)
     assert call(M=0) == call(n_seqs=0) == 0
-    for name in ("q", "kq", "kx", "vq", "vx", "out", "status"):
+    for name in ("q", "kq", "kx", "vq", "vx", "out", "scratch", "status"):
         assert call(**{name: None}) == BAD, name
     for over in (dict(n_seqs=-1), dict(M=-1), dict(n_heads=0), dict(n_kv_heads=0), dict(n_heads=6), dict(capacity=0)):
         assert call(**over) == BAD, over
     for over in (dict(capacity=40), dict(M=1 << 30), dict(n_seqs=1 << 20, capacity=1 << 12)):
         assert call(**over) == UNSUPPORTED, over
-    for name in ("q", "kq", "kx", "vq", "vx", "live", "out"):
+    for name in ("q", "kq", "kx", "vq", "vx", "live", "out", "scratch"):
         assert call(**{name: P + 8}) == MISALIGNED, name
     assert call(lens=P + 2) == call(status=P + 2) == MISALIGNED
+
+
+def test_attention_scratch(lib):
+    f = lib.ovggt_k_attention_q8_scratch_bytes
+    assert f(1, 1, 4, 4, 16) > 0                         # (a CTA takes it all: nothing to keep, but something to point to)
+    assert f(1, 1374, 16, 16, 17760) >= 2 * 17760 * 1024 * 2                      # both planes
+    assert f(64, 300, 16, 16, 17760) < 2 * f(1, 300, 16, 16, 17760)               # a few sequences at a time
+    for bad in ((0, 1, 4, 4, 16), (1, 0, 4, 4, 16), (1, 1, 0, 4, 16), (1, 1, 4, 0, 16), (1, 1, 6, 4, 16), (1, 1, 4, 4, 24), (1, 1, 4, 4, 0), (1, 1 << 30, 4, 4, 16)):
+        assert f(*bad) == 0, bad
