@@ -347,53 +347,197 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   return *reinterpret_cast<const uint32_t*>(&d);
 }
 
+// Where the live rows of each 64 of a sequence go among its live rows, and how many there are: they lie without gaps in the planes, so
+// the attention's loop knows no mask.  One CTA a sequence.
+constexpr int kWidenRows = 64;
+struct LiveArgs {
+  const int* lens;
+  const uint8_t* live;
+  int *first, *count;                  // [seqs, blocks], [seqs]
+  int cap, blocks;
+};
+__device__ __forceinline__ int q8_length(const int* lens, int seq, int cap) { return lens != nullptr ? min(cap, max(0, lens[seq])) : cap; }
+// A 64-row block's mask: bit r for row 64 block + r.
+__device__ __forceinline__ unsigned long long live_bits(const uint8_t* live, int len, int row0) {
+  unsigned long long bits = 0;
+#pragma unroll
+  for (int i = 0; i < kWidenRows / 16; ++i)
+    if (row0 + 16 * i < len) {                           // (the capacity is a multiple of 16)
+      const uint4 u = *reinterpret_cast<const uint4*>(live + row0 + 16 * i);
+      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t top = __vcmpne4(w[e], 0u) & 0x08040201u, nibble = (top | top >> 8 | top >> 16 | top >> 24) & 15u;
+        bits |= (unsigned long long)nibble << (16 * i + 4 * e);
+      }
+    }
+  const int left = len - row0;
+  return left >= kWidenRows ? bits : (left <= 0 ? 0ull : bits & ((1ull << left) - 1ull));
+}
+__global__ void __launch_bounds__(1024) k_live_rows(const LiveArgs P) {
+  __shared__ int sh[32];
+  pdl_trigger();
+  pdl_wait();
+  const int seq = blockIdx.x, len = q8_length(P.lens, seq, P.cap);
+  const uint8_t* live = P.live + (size_t)seq * P.cap;
+  int before = 0;
+  for (int b0 = 0; b0 < P.blocks; b0 += 1024) {
+    const int b = b0 + (int)threadIdx.x;
+    int total;
+    const int at = block_excl_scan_int(b < P.blocks ? __popcll(live_bits(live, len, b * kWidenRows)) : 0, sh, &total);
+    if (b < P.blocks) P.first[(size_t)seq * P.blocks + b] = before + at;
+    before += total;
+  }
+  if (threadIdx.x == 0) P.count[seq] = before;
+}
+
 struct WidenArgs {
   const uint4 *kq, *vq;                // [seqs, cap, HK * 64] int8
   const uint8_t *kx, *vx;
   const int* lens;
   const uint8_t* live;
+  const int *first, *count;            // of the live rows, where there is a mask
   uint4 *k, *v;                        // [seqs, rows, HK * 64] bf16
-  int seqs, cap, HK, rows;             // rows: the capacity up to whole tiles
+  unsigned* norms;                     // [seqs, rows / 64, HK]: the bits of the largest squared norm of a key of these rows, or nullptr
+  int cap, HK, rows;                   // rows: the capacity up to whole tiles
 };
 
-// Sixteen elements a thread; rows past the length, up to the end of its last tile, become zeros, as do values that are masked.  A
-// value whose key is not finite becomes NaN with it: its weight makes the result NaN whatever it comes out as.
+// A CTA takes 64 rows, sixteen elements a thread at a time, their exponents by way of shared memory.  Behind the last row, up to the end of
+// its tile, come zeros.  A value whose key is not finite becomes NaN with it: that makes the result NaN whatever its weight comes out as.
+constexpr int kWidenHeads = 256;       // heads whose exponents fit; with more (a row of 16384 elements) they are read where they are needed, and no norms taken
 __global__ void __launch_bounds__(256) k_widen_q8(const WidenArgs P) {
+  __shared__ uint8_t from[kWidenRows];                   // the live rows of this block, in order
+  __shared__ __align__(16) uint8_t sx[kWidenHeads][kWidenRows];
+  __shared__ unsigned top[kWidenHeads];
   pdl_trigger();
+  const int seq = blockIdx.y, side = blockIdx.z, row0 = (int)blockIdx.x * kWidenRows, units = P.HK * 4;
+  const bool norms = P.norms != nullptr && side == 0, staged = P.HK <= kWidenHeads;
   pdl_wait();
-  const int seq = blockIdx.y, side = blockIdx.z;
-  const long long at = (long long)blockIdx.x * 256 + threadIdx.x, block = at >> 2;
-  const long long row = block / P.HK;
-  const int h = (int)(block - row * P.HK);
-  const int len = min(P.cap, max(0, P.lens != nullptr ? P.lens[seq] : P.cap));
-  if (row >= (len + kBN - 1) / kBN * kBN) return;
-  uint4 w = make_uint4(0u, 0u, 0u, 0u);
-  uint32_t x = 0u;
-  if (row < len) {
-    w = ld_nc((side == 0 ? P.kq : P.vq) + (((size_t)seq * P.cap + row) * P.HK + h) * 4 + (at & 3));
-    const size_t xat = ((size_t)seq * P.HK + h) * P.cap + row;
-    x = P.kx[xat];
-    if (side == 1) x = P.live != nullptr && P.live[(size_t)seq * P.cap + row] == 0 ? 0u : (x == 255u ? 255u : P.vx[xat]);
+  const int len = q8_length(P.lens, seq, P.cap), count = P.live != nullptr ? P.count[seq] : len;
+  uint4* dst = (side == 0 ? P.k : P.v) + (size_t)seq * P.rows * units * 2;
+  const int have = max(0, min(kWidenRows, len - row0));
+  const uint8_t* kx = P.kx + (size_t)seq * P.HK * P.cap + row0;
+  const uint8_t* vx = P.vx + (size_t)seq * P.HK * P.cap + row0;
+  if (staged)
+    for (int i = threadIdx.x; i < units; i += 256) {     // (16 rows at a time: the capacity is a multiple of 16)
+      const int h = i >> 2, r = (i & 3) * 16;
+      if (r < have) {
+        uint4 x = *reinterpret_cast<const uint4*>(kx + (size_t)h * P.cap + r);
+        if (side == 1) {
+          const uint4 y = *reinterpret_cast<const uint4*>(vx + (size_t)h * P.cap + r);
+          x.x = y.x | __vcmpeq4(x.x, 0xFFFFFFFFu);
+          x.y = y.y | __vcmpeq4(x.y, 0xFFFFFFFFu);
+          x.z = y.z | __vcmpeq4(x.z, 0xFFFFFFFFu);
+          x.w = y.w | __vcmpeq4(x.w, 0xFFFFFFFFu);
+        }
+        *reinterpret_cast<uint4*>(&sx[h][r]) = x;
+      }
+    }
+  if (norms)
+    for (int h = threadIdx.x; h < P.HK; h += 256) top[h] = 0u;
+  int n = have, to = row0;
+  if (P.live != nullptr) {
+    if (threadIdx.x < 32) {
+      const unsigned long long bits = live_bits(P.live + (size_t)seq * P.cap, len, row0);
+      for (int r = threadIdx.x; r < kWidenRows; r += 32)
+        if (bits >> r & 1ull) from[__popcll(bits & ((1ull << r) - 1ull))] = (uint8_t)r;
+    }
+    to = P.first[(size_t)seq * gridDim.x + blockIdx.x];
+    n = (blockIdx.x + 1 < gridDim.x ? P.first[(size_t)seq * gridDim.x + blockIdx.x + 1] : count) - to;
   }
-  const uint32_t step = q8_step_bf16x2(x), in[4] = {w.x, w.y, w.z, w.w};
-  uint32_t o[8];
+  __syncthreads();
+  const uint4* src = (side == 0 ? P.kq : P.vq) + ((size_t)seq * P.cap + row0) * units;
+  uint4* d = dst + (size_t)to * units * 2;
+  const bool steady = 256 % units == 0;                  // a thread's head stays the same
+  unsigned most = 0u;
+  auto widen = [&](const uint4& w, int part, int r, int u) {
+    uint32_t x;
+    if (staged) {
+      x = sx[part >> 2][r];
+    } else {
+      x = kx[(size_t)(part >> 2) * P.cap + r];
+      if (side == 1 && x != 255u) x = vx[(size_t)(part >> 2) * P.cap + r];
+    }
+    const uint32_t step = q8_step_bf16x2(x), in[4] = {w.x, w.y, w.z, w.w};
+    uint32_t o[8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    o[2 * i] = mul_bf16x2(int8_to_bf16x2(__byte_perm(in[i], 0x43434343u, 0x4140)), step);
-    o[2 * i + 1] = mul_bf16x2(int8_to_bf16x2(__byte_perm(in[i], 0x43434343u, 0x4342)), step);
+    for (int e = 0; e < 4; ++e) {
+      o[2 * e] = mul_bf16x2(int8_to_bf16x2(__byte_perm(in[e], 0x43434343u, 0x4140)), step);
+      o[2 * e + 1] = mul_bf16x2(int8_to_bf16x2(__byte_perm(in[e], 0x43434343u, 0x4342)), step);
+    }
+    d[2 * u] = make_uint4(o[0], o[1], o[2], o[3]);
+    d[2 * u + 1] = make_uint4(o[4], o[5], o[6], o[7]);
+    if (norms) {                                         // (four lanes have a key of a head: whole numbers of at most 64 x 127^2)
+      int n2 = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) n2 = __dp4a((int)in[e], (int)in[e], n2);
+      const unsigned quad = 15u << (threadIdx.x & 28);
+      n2 += __shfl_xor_sync(quad, n2, 1);
+      n2 += __shfl_xor_sync(quad, n2, 2);
+      const float f = q8_step(x);
+      most = max(most, __float_as_uint((float)n2 * f * f) & 0x7FFFFFFFu);
+      if (!steady && (part & 3) == 0) {
+        atomicMax(&top[part >> 2], most);
+        most = 0u;
+      }
+    }
+  };
+  const int all = n * units, i_step = 256 / units, part_step = 256 % units;
+  int i = (int)threadIdx.x / units, part = (int)threadIdx.x % units;
+#pragma unroll 1
+  for (int u = threadIdx.x; u < all;) {
+    constexpr int kAtOnce = 4;                           // a thread's loads on their way together
+    uint4 w[kAtOnce];
+    int parts[kAtOnce], rs[kAtOnce];
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) {
+      parts[j] = part;
+      rs[j] = 0;
+      if (u + 256 * j < all) {
+        rs[j] = P.live != nullptr ? from[i] : i;
+        w[j] = ld_nc(src + (size_t)rs[j] * units + part);
+      }
+      i += i_step, part += part_step;
+      if (part >= units) part -= units, ++i;
+    }
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j, u += 256)
+      if (u < all) widen(w[j], parts[j], rs[j], u);
   }
-  uint4* d = (side == 0 ? P.k : P.v) + (size_t)seq * P.rows * P.HK * 8 + 2 * (size_t)at;
-  d[0] = make_uint4(o[0], o[1], o[2], o[3]);
-  d[1] = make_uint4(o[4], o[5], o[6], o[7]);
+  if (norms) {
+    if (steady && most != 0u && ((int)threadIdx.x & 3) == 0) atomicMax(&top[(int)threadIdx.x % units >> 2], most);
+    __syncthreads();
+    for (int h = threadIdx.x; h < P.HK; h += 256) P.norms[((size_t)seq * gridDim.x + blockIdx.x) * P.HK + h] = top[h];
+  }
+  // this CTA's share of the zeros: rows [row0, row0 + 64) of the planes
+  const int z0 = max(row0, count), z1 = min(row0 + kWidenRows, (count + kBN - 1) / kBN * kBN);
+  for (int u = threadIdx.x; u < (z1 - z0) * units * 2; u += 256) dst[(size_t)z0 * units * 2 + u] = make_uint4(0u, 0u, 0u, 0u);
 }
 
-// The bf16 attention's scheme (see attn_tcgen05.cuh: the same warps, tiles, halves and order of MMAs, two CTAs an SM) with lengths and masks
-// that are read here, sequences and shared heads, and rows without a live cached row.
+// The bf16 attention's scheme (see attn_tcgen05.cuh: the same warps, tiles, halves and order of MMAs, two CTAs an SM) with lengths that are
+// read here, sequences and shared heads, and sequences without a live row.
 constexpr int kManyBar = kQBytes + 2 * kKVStages * kTileBytes;
 constexpr int kManySmem = kManyBar + (int)sizeof(AttnBarriers) + 64;
 
+// What a CTA takes: a tile of rows, a key head, a part of the cached rows, a sequence.
+struct Place {
+  int row0, hk, part, seq;
+  __device__ __forceinline__ Place(const AttnQ8Args& P, unsigned block) {
+    const unsigned a = block / P.q_tiles, b = a / P.HK;
+    row0 = (int)(block - a * P.q_tiles) * kBM;
+    hk = (int)(a - b * P.HK);
+    seq = (int)(b / P.parts);
+    part = (int)(b - (unsigned)seq * P.parts);
+  }
+  // Where row r lies in q and out: it is token r / group, head r % group of this group.
+  __device__ __forceinline__ size_t q(const AttnQ8Args& P, int r) const {
+    const int m = r / P.group;
+    return (((size_t)seq * P.M + m) * P.H + (size_t)hk * P.group + (r - m * P.group)) * kHD;
+  }
+};
+
 __global__ void __launch_bounds__(kAttnThreads, kCtasPerSm)
-k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ AttnQ8Args P, const int plane_rows) {
+k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ AttnQ8Args P, const int* counts, const unsigned* norms, const int plane_rows) {
   extern __shared__ __align__(1024) unsigned char smem[];
   if (smem_u32(smem) & 1023u) {                          // the 128-byte swizzle needs 1024-byte aligned tiles
     if (threadIdx.x == 0) report_status(P.status, OVGGT_ERR_DEVICE_STATUS);
@@ -403,14 +547,11 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
   unsigned char* sK = sQ + kQBytes;
   unsigned char* sV = sK + kKVStages * kTileBytes;
   AttnBarriers* B = reinterpret_cast<AttnBarriers*>(smem + kManyBar);
+  unsigned* top = reinterpret_cast<unsigned*>(B + 1);    // [4]
+  volatile int* range = reinterpret_cast<volatile int*>(top + 4);             // halves of this CTA, live rows from its first tile on: read where they are needed
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int qt = (int)(blockIdx.x % P.q_tiles), hk = (int)(blockIdx.x / P.q_tiles % P.HK), rest = (int)(blockIdx.x / P.q_tiles / P.HK);
-  const int part = rest % P.parts, seq = rest / P.parts;
-  const int rows = P.M * P.group, row0 = qt * kBM;
-  auto q_at = [&](int r) {                               // (row r is token r / group, head r % group of this group)
-    const int m = r / P.group;
-    return (((size_t)seq * P.M + m) * P.H + (size_t)hk * P.group + (r - m * P.group)) * kHD;
-  };
+  const Place at0(P, blockIdx.x);
+  const int hk = at0.hk, part = at0.part, seq = at0.seq;
   pdl_trigger();
   if (warp == 4 && lane == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_k) : "memory");
@@ -437,7 +578,7 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   pdl_wait();
-  const int len = min(P.cap, max(0, P.lens != nullptr ? P.lens[seq] : P.cap));
+  const int len = counts != nullptr ? counts[seq] : q8_length(P.lens, seq, P.cap);      // live rows
   const int tiles_total = (len + kBN - 1) / kBN;
   const int t_begin = (int)((long long)part * tiles_total / P.parts), n_tiles = (int)((long long)(part + 1) * tiles_total / P.parts) - t_begin;
   {                                                      // Q: 128 rows x 8 groups of 8 columns, rows past the last zero
@@ -445,14 +586,25 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
     uint4 x[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int idx = threadIdx.x + i * kAttnThreads, r = row0 + (idx >> 3);
-      x[i] = r < rows ? *reinterpret_cast<const uint4*>(P.q + q_at(r) + (idx & 7) * 8) : make_uint4(0u, 0u, 0u, 0u);
+      const int idx = threadIdx.x + i * kAttnThreads, r = at0.row0 + (idx >> 3);
+      x[i] = r < P.M * P.group ? *reinterpret_cast<const uint4*>(P.q + at0.q(P, r) + (idx & 7) * 8) : make_uint4(0u, 0u, 0u, 0u);
     }
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int idx = threadIdx.x + i * kAttnThreads, r = idx >> 3;
       *reinterpret_cast<uint4*>(sQ + r * 128 + (((idx & 7) ^ (r & 7)) << 4)) = x[i];
     }
+  }
+  if (threadIdx.x == 0) {
+    range[0] = 2 * n_tiles;
+    range[1] = len - t_begin * kBN;
+  }
+  if (warp < 4 && norms != nullptr) {                    // the largest squared norm of this head's keys
+    unsigned most = 0u;
+    const int blocks = (q8_length(P.lens, seq, P.cap) + kWidenRows - 1) / kWidenRows;
+    for (int b = threadIdx.x; b < blocks; b += 128) most = max(most, norms[((size_t)seq * (plane_rows / kWidenRows) + b) * P.HK + hk]);
+    most = __reduce_max_sync(0xFFFFFFFFu, most);
+    if (lane == 0) top[warp] = most;
   }
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   tc_fence_before();
@@ -558,23 +710,28 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
     const uint32_t t_row = tmem + ((uint32_t)(warp * 32) << 16);
     const float c = 1.4426950408889634f * 0.125f;        // log2(e) / sqrt(64)
     float m = -INFINITY, l = 0.0f;
-    bool ok = true, seen = false;                        // seen: some cached row is live
-    for (int idx = 0; idx < 2 * n_tiles && ok; ++idx) {  // idx = 2 * tile + half
-      const int it = idx >> 1, hf = idx & 1, col0 = (t_begin + it) * kBN + hf * kHalf;
-      uint32_t mask[kHalf / 32];
-      bool whole = P.live == nullptr && col0 + kHalf <= len;
-      if (!whole) {
-        whole = true;
+    bool ok = true;
+    // Upper bound of this row's logits in log2 units, |q| |k|_max log2(e) / 8, for the fixed reference (see attn_tcgen05.cuh).
+    float bound = INFINITY;
+    bool fixed_ref = false, in_range = false;
+    if (norms != nullptr) {
+      const float kmax2 = __uint_as_float(max(max(top[0], top[1]), max(top[2], top[3])));
+      float qn2 = 0.0f;
 #pragma unroll
-        for (int j = 0; j < kHalf / 32; ++j) {
-          const int r = col0 + 32 * j + lane;
-          mask[j] = __ballot_sync(0xFFFFFFFFu, r < len && (P.live == nullptr || P.live[(size_t)seq * P.cap + r] != 0));
-          whole = whole && mask[j] == 0xFFFFFFFFu;
-          seen = seen || mask[j] != 0u;
+      for (int j = 0; j < 8; ++j) {
+        const uint4 u = *reinterpret_cast<const uint4*>(sQ + row * 128 + ((j ^ (row & 7)) << 4));
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float lo = __uint_as_float(w[e] << 16), hi = __uint_as_float(w[e] & 0xFFFF0000u);
+          qn2 = fmaf(lo, lo, qn2);
+          qn2 = fmaf(hi, hi, qn2);
         }
-      } else {
-        seen = true;
       }
+      bound = sqrtf(qn2 * kmax2) * c;
+    }
+    for (int idx = 0; idx < range[0] && ok; ++idx) {    // idx = 2 * tile + half
+      const int it = idx >> 1, hf = idx & 1;
       // (every wait result is made warp-uniform before the warp meets an .aligned tensor-memory instruction)
       ok = __all_sync(0xFFFFFFFFu, mbar_wait(&B->s_full[hf], (uint32_t)it & 1u, B, P.status)) != 0;
       if (!ok) break;
@@ -584,16 +741,16 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
 #pragma unroll
         for (int j = 0; j < kHalf / 32; ++j) tmem_ld32(t_row + kColS + hf * kHalf + j * 32, s + j * 32);
         tmem_wait_ld();
-        if (!whole) {
+        const int left = range[1] - idx * kHalf;
+        if (left < kHalf) {
 #pragma unroll
           for (int j = 0; j < kHalf; ++j)
-            if (!(mask[j >> 5] >> (j & 31) & 1u)) s[j] = 0xFF800000u;
+            if (j >= left) s[j] = 0xFF800000u;           // -inf on columns past the last row
         }
       };
       // p = 2^(s c - reference) on pairs, packed to bf16 over the front of s[]; returns the row's sum of p and its largest raw score
-      auto exp_pass = [&](auto track, float& raw) -> float {
-        const float ref = m == -INFINITY ? 0.0f : m;
-        const float2 c2 = make_float2(c, c), nm2 = make_float2(-ref, -ref);
+      auto exp_pass = [&](auto track, auto clamp, float& raw) -> float {
+        const float2 c2 = make_float2(c, c), nm2 = make_float2(-m, -m);
         float2 acc[4];
         float m4[4];
 #pragma unroll
@@ -606,7 +763,7 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
           const float s0 = __uint_as_float(s[j]), s1 = __uint_as_float(s[j + 1]);
           if constexpr (decltype(track)::value) m4[(j >> 1) & 3] = max3(m4[(j >> 1) & 3], s0, s1);
           const float2 x = fma2(make_float2(s0, s1), c2, nm2);
-          const float2 p = pair_on_fma_pipes(j >> 1) ? ex2_poly2<true>(x) : make_float2(ex2(x.x), ex2(x.y));
+          const float2 p = pair_on_fma_pipes(j >> 1) ? ex2_poly2<decltype(clamp)::value>(x) : make_float2(ex2(x.x), ex2(x.y));
           acc[(j >> 1) & 3] = add2(acc[(j >> 1) & 3], p);
           s[j >> 1] = pack_bf16(p.x, p.y);
         }
@@ -627,14 +784,20 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
           for (int j = 2; j < kChain; j += 2) m4[q] = max3(m4[q], __uint_as_float(s[kChain * q + j]), __uint_as_float(s[kChain * q + j + 1]));
         }
         m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * c;
-        add = exp_pass(std::false_type{}, raw);
+        // the bound as the reference, a whole number of powers of two above what was seen, where it is not absurdly far above
+        fixed_ref = __all_sync(0xFFFFFFFFu, bound >= m && bound - m <= kFixedRefMaxGap) != 0;
+        if (fixed_ref) m += ceilf(bound - m);
+        in_range = fixed_ref && __all_sync(0xFFFFFFFFu, bound + m <= -1.0f - kPolyLowest) != 0;
+        add = exp_pass(std::false_type{}, std::true_type{}, raw);
+      } else if (fixed_ref) {
+        add = in_range && (idx + 1) * kHalf <= range[1] ? exp_pass(std::false_type{}, std::false_type{}, raw) : exp_pass(std::false_type{}, std::true_type{}, raw);
       } else {
-        add = exp_pass(std::true_type{}, raw);
+        add = exp_pass(std::true_type{}, std::true_type{}, raw);
         const float mx = raw * c;
-        const bool grow = mx - m > kRescaleThreshold;    // (also from nothing live to something)
+        const bool grow = mx - m > kRescaleThreshold;
         if (__any_sync(0xFFFFFFFFu, grow)) {
           // O may still be accumulating the half before: the scores of the next half, issued behind it, tell; or the last one's own barrier
-          ok = idx + 1 < 2 * n_tiles ? mbar_wait(&B->s_full[hf ^ 1], (uint32_t)((idx + 1) >> 1) & 1u, B, P.status)
+          ok = idx + 1 < range[0] ? mbar_wait(&B->s_full[hf ^ 1], (uint32_t)((idx + 1) >> 1) & 1u, B, P.status)
                                      : mbar_wait(&B->pv_done, 0, B, P.status);
           ok = __all_sync(0xFFFFFFFFu, ok) != 0;
           if (!ok) break;
@@ -654,7 +817,7 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
             tmem_st16(t_row + kColO + j * 16, o);
           }
           load_scores();
-          add = exp_pass(std::false_type{}, raw);
+          add = exp_pass(std::false_type{}, std::true_type{}, raw);
         }
       }
       l += add;
@@ -664,11 +827,12 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
       tc_fence_before();
       mbar_arrive(&B->p_full[hf]);
     }
-    if (n_tiles > 0 && ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&B->o_full, 0, B, P.status)) != 0;
+    const bool seen = range[0] > 0;
+    if (seen && ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&B->o_full, 0, B, P.status)) != 0;
     if (ok) {
       tc_fence_after();
-      // Live rows, but no score that is a number, or one that is infinite: not a number.
-      if ((seen && m == -INFINITY) || m == INFINITY) l = __int_as_float(0x7FC00000);
+      // (a tile's first half has a live row: a maximum of -inf is one of scores that are not numbers, and an infinite one makes NaN too)
+      if (seen && fabsf(m) == INFINITY) l = __int_as_float(0x7FC00000);
       const bool one = P.parts == 1;
       const float inv = !seen ? 0.0f : (one ? 1.0f / l : 1.0f);
       // By way of the operand tiles, which are free now: a thread has a row, but a warp stores whole lines of it.
@@ -676,7 +840,7 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         uint32_t o[32];
-        if (n_tiles > 0) {
+        if (seen) {
           tmem_ld32(t_row + kColO + j * 32, o);
           tmem_wait_ld();
         }
@@ -695,18 +859,22 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
         }
       }
       __syncwarp();
-      const size_t shift = (size_t)part * P.seqs * P.M * P.H * kHD;
+      unsigned block = blockIdx.x;
+      asm volatile("" : "+r"(block));                    // (taken apart again: nothing of it is kept through the loop)
+      const Place at1(P, block);
+      const int rows = P.M * P.group, row0 = at1.row0;
+      const size_t shift = (size_t)at1.part * P.seqs * P.M * P.H * kHD;
       const int words = one ? 8 : 16;                    // 16-byte words of a row
 #pragma unroll 4
       for (int u = lane; u < 32 * words; u += 32) {
         const int r = u / words, w = u - r * words, at_row = row0 + warp * 32 + r;
         if (at_row < rows) {
           const uint4 x = *reinterpret_cast<const uint4*>(stage + r * kOutRow + w * 16);
-          if (one) *reinterpret_cast<uint4*>(P.out + q_at(at_row) + w * 8) = x;
-          else *reinterpret_cast<uint4*>(P.o_part + shift + q_at(at_row) + w * 4) = x;
+          if (one) *reinterpret_cast<uint4*>(P.out + at1.q(P, at_row) + w * 8) = x;
+          else *reinterpret_cast<uint4*>(P.o_part + shift + at1.q(P, at_row) + w * 4) = x;
         }
       }
-      if (!one && row0 + row < rows) P.ml_part[(shift + q_at(row0 + row)) / kHD] = make_float2(seen && m != -INFINITY ? m : kDeadMax, seen ? l : kDeadSum);
+      if (!one && row0 + row < rows) P.ml_part[(shift + at1.q(P, row0 + row)) / kHD] = seen ? make_float2(fmaxf(m, kDeadMax), l) : make_float2(kDeadMax, kDeadSum);
     }
   }
 
@@ -726,7 +894,7 @@ constexpr int kManyFrom = 65;          // rows from which the planes are taken
 // How a call is cut: rows a CTA takes (8, 16, 32: the few-row kernel; 128), parts of the cached rows, sequences at once.
 struct AttnQ8Plan {
   int tile, q_tiles, parts, seqs, plane_rows;
-  size_t planes, o_part, bytes;        // of scratch: K and V planes, the parts' results, all
+  size_t planes, o_part, ml_part, bytes;   // of scratch: K and V planes, the parts' results, where the live rows go and the norms; all
 };
 inline AttnQ8Plan attn_q8_plan(int seqs, int M, int H, int HK, int cap) {
   AttnQ8Plan A = {};
@@ -755,7 +923,8 @@ inline AttnQ8Plan attn_q8_plan(int seqs, int M, int H, int HK, int cap) {
     A.parts = (int)std::max(1ll, std::min({(long long)kMaxSplits, places / jobs, most}));
   }
   A.o_part = A.parts == 1 ? 0 : (size_t)A.parts * A.seqs * M * H * kHD * 4;
-  A.bytes = A.planes + A.o_part + (A.parts == 1 ? 0 : (size_t)A.parts * A.seqs * M * H * 8);
+  A.ml_part = A.parts == 1 ? 0 : (size_t)A.parts * A.seqs * M * H * 8;
+  A.bytes = A.planes + A.o_part + A.ml_part + (A.planes ? (size_t)A.seqs * (A.plane_rows / kWidenRows * (1 + (HK <= kWidenHeads ? HK : 0)) + 1) * 4 : 0);
   return A;
 }
 
@@ -776,18 +945,26 @@ static inline int attn_q8_launch(AttnQ8Args P, void* scratch, cudaStream_t st, i
     if (A.tile == kBM) {
       char* planes = static_cast<char*>(scratch);
       const size_t side = A.planes / 2;
-      const WidenArgs W = {reinterpret_cast<const uint4*>(P.kq), reinterpret_cast<const uint4*>(P.vq), P.kx, P.vx, P.lens, P.live,
-                           reinterpret_cast<uint4*>(planes), reinterpret_cast<uint4*>(planes + side), P.seqs, P.cap, P.HK, A.plane_rows};
+      const int blocks = A.plane_rows / kWidenRows;
+      int* first = reinterpret_cast<int*>(planes + A.planes + A.o_part + A.ml_part);
+      int* counts = P.live ? first + (size_t)A.seqs * blocks : nullptr;
+      unsigned* norms = P.HK <= kWidenHeads ? reinterpret_cast<unsigned*>(first + (size_t)A.seqs * (blocks + 1)) : nullptr;
+      const WidenArgs W = {reinterpret_cast<const uint4*>(P.kq), reinterpret_cast<const uint4*>(P.vq), P.kx, P.vx, P.lens, P.live, first, counts,
+                           reinterpret_cast<uint4*>(planes), reinterpret_cast<uint4*>(planes + side), norms, P.cap, P.HK, A.plane_rows};
       CUtensorMap tk, tv;
       int rc = make_rows_map(&tk, planes, P.seqs * A.plane_rows, P.HK * kHD, kBN);
       if (rc) return rc;
       rc = make_rows_map(&tv, planes + side, P.seqs * A.plane_rows, P.HK * kHD, kBN);
       if (rc) return rc;
-      const long long widen = ((long long)A.plane_rows * P.HK * 4 + 255) / 256;
-      e = launch_dependent(k_widen_q8, dim3((unsigned)widen, P.seqs, 2), 256, 1, 0, st, true, W);
+      e = cudaSuccess;
+      if (P.live) {
+        e = launch_dependent(k_live_rows, dim3(P.seqs), 1024, 1, 0, st, true, LiveArgs{P.lens, P.live, first, counts, P.cap, blocks});
+        *launches += 1;
+      }
+      if (e == cudaSuccess) e = launch_dependent(k_widen_q8, dim3(blocks, P.seqs, 2), 256, 1, 0, st, true, W);
       static std::atomic<uint64_t> smem_many;
       if (e == cudaSuccess) e = allow_smem(k_attn_q8_many, kManySmem, smem_many);
-      if (e == cudaSuccess) e = launch_dependent(k_attn_q8_many, dim3((unsigned)ctas), kAttnThreads, 1, kManySmem, st, true, tk, tv, P, A.plane_rows);
+      if (e == cudaSuccess) e = launch_dependent(k_attn_q8_many, dim3((unsigned)ctas), kAttnThreads, 1, kManySmem, st, true, tk, tv, P, (const int*)counts, (const unsigned*)norms, A.plane_rows);
       *launches += 2;
     } else {
       const auto kernel = A.tile == 8 ? k_attn_q8_few<8> : (A.tile == 16 ? k_attn_q8_few<16> : k_attn_q8_few<32>);
