@@ -398,120 +398,99 @@ struct WidenArgs {
   const uint8_t* live;
   const int *first, *count;            // of the live rows, where there is a mask
   uint4 *k, *v;                        // [seqs, rows, HK * 64] bf16
-  unsigned* norms;                     // [seqs, rows / 64, HK]: the bits of the largest squared norm of a key of these rows, or nullptr
+  unsigned* norms;                     // [seqs, rows / 64, HK]: the bits of the largest squared norm of a key of these rows
   int cap, HK, rows;                   // rows: the capacity up to whole tiles
 };
 
-// A CTA takes 64 rows, sixteen elements a thread at a time, their exponents by way of shared memory.  Behind the last row, up to the end of
-// its tile, come zeros.  A value whose key is not finite becomes NaN with it: that makes the result NaN whatever its weight comes out as.
-constexpr int kWidenHeads = 256;       // heads whose exponents fit; with more (a row of 16384 elements) they are read where they are needed, and no norms taken
+// A CTA takes 64 rows of four heads, sixteen elements a thread at a time, their exponents by way of shared memory: all of a thread's loads are
+// on their way at once (17758 rows of 16 heads: 23.6 us with all heads in a CTA).  Behind the last row, up to the end of its tile, come zeros.  A value
+// whose key is not finite becomes NaN with it: that makes the result NaN whatever its weight comes out as.
+constexpr int kWidenHeads = 4, kWidenUnits = kWidenRows * kWidenHeads * 4 / 256;   // heads of a CTA, units of a thread
 __global__ void __launch_bounds__(256) k_widen_q8(const WidenArgs P) {
   __shared__ uint8_t from[kWidenRows];                   // the live rows of this block, in order
   __shared__ __align__(16) uint8_t sx[kWidenHeads][kWidenRows];
   __shared__ unsigned top[kWidenHeads];
   pdl_trigger();
-  const int seq = blockIdx.y, side = blockIdx.z, row0 = (int)blockIdx.x * kWidenRows, units = P.HK * 4;
-  const bool norms = P.norms != nullptr && side == 0, staged = P.HK <= kWidenHeads;
+  const int seq = blockIdx.y, side = blockIdx.z & 1, h0 = (int)(blockIdx.z >> 1) * kWidenHeads, row0 = (int)blockIdx.x * kWidenRows;
+  const int heads = min(kWidenHeads, P.HK - h0), units = heads * 4;               // of a row here
+  const size_t pitch = (size_t)P.HK * 4;                 // 16-byte words of a cached row
+  if (threadIdx.x < kWidenHeads) top[threadIdx.x] = 0u;
   pdl_wait();
-  const int len = q8_length(P.lens, seq, P.cap), count = P.live != nullptr ? P.count[seq] : len;
-  uint4* dst = (side == 0 ? P.k : P.v) + (size_t)seq * P.rows * units * 2;
+  const int len = q8_length(P.lens, seq, P.cap);
   const int have = max(0, min(kWidenRows, len - row0));
-  const uint8_t* kx = P.kx + (size_t)seq * P.HK * P.cap + row0;
-  const uint8_t* vx = P.vx + (size_t)seq * P.HK * P.cap + row0;
-  if (staged)
-    for (int i = threadIdx.x; i < units; i += 256) {     // (16 rows at a time: the capacity is a multiple of 16)
-      const int h = i >> 2, r = (i & 3) * 16;
-      if (r < have) {
-        uint4 x = *reinterpret_cast<const uint4*>(kx + (size_t)h * P.cap + r);
-        if (side == 1) {
-          const uint4 y = *reinterpret_cast<const uint4*>(vx + (size_t)h * P.cap + r);
-          x.x = y.x | __vcmpeq4(x.x, 0xFFFFFFFFu);
-          x.y = y.y | __vcmpeq4(x.y, 0xFFFFFFFFu);
-          x.z = y.z | __vcmpeq4(x.z, 0xFFFFFFFFu);
-          x.w = y.w | __vcmpeq4(x.w, 0xFFFFFFFFu);
-        }
-        *reinterpret_cast<uint4*>(&sx[h][r]) = x;
-      }
-    }
-  if (norms)
-    for (int h = threadIdx.x; h < P.HK; h += 256) top[h] = 0u;
-  int n = have, to = row0;
+  int n = have, to = row0, count = len;
   if (P.live != nullptr) {
-    if (threadIdx.x < 32) {
+    count = P.count[seq];
+    if (threadIdx.x >= 224) {
       const unsigned long long bits = live_bits(P.live + (size_t)seq * P.cap, len, row0);
-      for (int r = threadIdx.x; r < kWidenRows; r += 32)
+      for (int r = threadIdx.x - 224; r < kWidenRows; r += 32)
         if (bits >> r & 1ull) from[__popcll(bits & ((1ull << r) - 1ull))] = (uint8_t)r;
     }
     to = P.first[(size_t)seq * gridDim.x + blockIdx.x];
     n = (blockIdx.x + 1 < gridDim.x ? P.first[(size_t)seq * gridDim.x + blockIdx.x + 1] : count) - to;
+    __syncthreads();
+  }
+  const int all = n * units;
+  const uint4* src = (side == 0 ? P.kq : P.vq) + ((size_t)seq * P.cap + row0) * pitch + h0 * 4;
+  uint4 w[kWidenUnits];
+#pragma unroll
+  for (int j = 0; j < kWidenUnits; ++j) {
+    const int u = threadIdx.x + 256 * j, i = u / units;
+    if (u < all) w[j] = ld_nc(src + (P.live != nullptr ? from[i] : i) * pitch + (u - i * units));
+  }
+  if ((int)threadIdx.x < units) {                        // (16 rows at a time: the capacity is a multiple of 16)
+    const int h = threadIdx.x >> 2, r = (threadIdx.x & 3) * 16;
+    if (r < have) {
+      const size_t at = ((size_t)seq * P.HK + h0 + h) * P.cap + row0 + r;
+      uint4 x = *reinterpret_cast<const uint4*>(P.kx + at);
+      if (side == 1) {
+        const uint4 y = *reinterpret_cast<const uint4*>(P.vx + at);
+        x.x = y.x | __vcmpeq4(x.x, 0xFFFFFFFFu);
+        x.y = y.y | __vcmpeq4(x.y, 0xFFFFFFFFu);
+        x.z = y.z | __vcmpeq4(x.z, 0xFFFFFFFFu);
+        x.w = y.w | __vcmpeq4(x.w, 0xFFFFFFFFu);
+      }
+      *reinterpret_cast<uint4*>(&sx[h][r]) = x;
+    }
   }
   __syncthreads();
-  const uint4* src = (side == 0 ? P.kq : P.vq) + ((size_t)seq * P.cap + row0) * units;
-  uint4* d = dst + (size_t)to * units * 2;
-  const bool steady = 256 % units == 0;                  // a thread's head stays the same
-  unsigned most = 0u;
-  auto widen = [&](const uint4& w, int part, int r, int u) {
-    uint32_t x;
-    if (staged) {
-      x = sx[part >> 2][r];
-    } else {
-      x = kx[(size_t)(part >> 2) * P.cap + r];
-      if (side == 1 && x != 255u) x = vx[(size_t)(part >> 2) * P.cap + r];
-    }
-    const uint32_t step = q8_step_bf16x2(x), in[4] = {w.x, w.y, w.z, w.w};
-    uint32_t o[8];
+  uint4* dst = (side == 0 ? P.k : P.v) + (size_t)seq * P.rows * pitch * 2 + h0 * 8;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      o[2 * e] = mul_bf16x2(int8_to_bf16x2(__byte_perm(in[e], 0x43434343u, 0x4140)), step);
-      o[2 * e + 1] = mul_bf16x2(int8_to_bf16x2(__byte_perm(in[e], 0x43434343u, 0x4342)), step);
-    }
-    d[2 * u] = make_uint4(o[0], o[1], o[2], o[3]);
-    d[2 * u + 1] = make_uint4(o[4], o[5], o[6], o[7]);
-    if (norms) {                                         // (four lanes have a key of a head: whole numbers of at most 64 x 127^2)
-      int n2 = 0;
+  for (int j = 0; j < kWidenUnits; ++j) {
+    const int u = threadIdx.x + 256 * j, i = u / units, part = u - i * units;
+    if (u < all) {
+      const uint32_t x = sx[part >> 2][P.live != nullptr ? from[i] : i], step = q8_step_bf16x2(x), in[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+      uint32_t o[8];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) n2 = __dp4a((int)in[e], (int)in[e], n2);
-      const unsigned quad = 15u << (threadIdx.x & 28);
-      n2 += __shfl_xor_sync(quad, n2, 1);
-      n2 += __shfl_xor_sync(quad, n2, 2);
-      const float f = q8_step(x);
-      most = max(most, __float_as_uint((float)n2 * f * f) & 0x7FFFFFFFu);
-      if (!steady && (part & 3) == 0) {
-        atomicMax(&top[part >> 2], most);
-        most = 0u;
+      for (int e = 0; e < 4; ++e) {
+        o[2 * e] = mul_bf16x2(int8_to_bf16x2(__byte_perm(in[e], 0x43434343u, 0x4140)), step);
+        o[2 * e + 1] = mul_bf16x2(int8_to_bf16x2(__byte_perm(in[e], 0x43434343u, 0x4342)), step);
+      }
+      uint4* d = dst + (size_t)(to + i) * pitch * 2 + 2 * part;
+      d[0] = make_uint4(o[0], o[1], o[2], o[3]);
+      d[1] = make_uint4(o[4], o[5], o[6], o[7]);
+      if (side == 0) {                                   // (four lanes have a key of a head: whole numbers of at most 64 x 127^2)
+        int n2 = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) n2 = __dp4a((int)in[e], (int)in[e], n2);
+        const unsigned quad = 15u << (threadIdx.x & 28);
+        n2 += __shfl_xor_sync(quad, n2, 1);
+        n2 += __shfl_xor_sync(quad, n2, 2);
+        const float f = q8_step(x);
+        if ((part & 3) == 0) atomicMax(&top[part >> 2], __float_as_uint((float)n2 * f * f) & 0x7FFFFFFFu);
       }
     }
-  };
-  const int all = n * units, i_step = 256 / units, part_step = 256 % units;
-  int i = (int)threadIdx.x / units, part = (int)threadIdx.x % units;
-#pragma unroll 1
-  for (int u = threadIdx.x; u < all;) {
-    constexpr int kAtOnce = 4;                           // a thread's loads on their way together
-    uint4 w[kAtOnce];
-    int parts[kAtOnce], rs[kAtOnce];
-#pragma unroll
-    for (int j = 0; j < kAtOnce; ++j) {
-      parts[j] = part;
-      rs[j] = 0;
-      if (u + 256 * j < all) {
-        rs[j] = P.live != nullptr ? from[i] : i;
-        w[j] = ld_nc(src + (size_t)rs[j] * units + part);
-      }
-      i += i_step, part += part_step;
-      if (part >= units) part -= units, ++i;
-    }
-#pragma unroll
-    for (int j = 0; j < kAtOnce; ++j, u += 256)
-      if (u < all) widen(w[j], parts[j], rs[j], u);
   }
-  if (norms) {
-    if (steady && most != 0u && ((int)threadIdx.x & 3) == 0) atomicMax(&top[(int)threadIdx.x % units >> 2], most);
+  if (side == 0) {
     __syncthreads();
-    for (int h = threadIdx.x; h < P.HK; h += 256) P.norms[((size_t)seq * gridDim.x + blockIdx.x) * P.HK + h] = top[h];
+    if ((int)threadIdx.x < heads) P.norms[((size_t)seq * gridDim.x + blockIdx.x) * P.HK + h0 + threadIdx.x] = top[threadIdx.x];
   }
   // this CTA's share of the zeros: rows [row0, row0 + 64) of the planes
   const int z0 = max(row0, count), z1 = min(row0 + kWidenRows, (count + kBN - 1) / kBN * kBN);
-  for (int u = threadIdx.x; u < (z1 - z0) * units * 2; u += 256) dst[(size_t)z0 * units * 2 + u] = make_uint4(0u, 0u, 0u, 0u);
+  for (int u = threadIdx.x; u < (z1 - z0) * units * 2; u += 256) {
+    const int i = u / (units * 2);
+    dst[(size_t)(z0 + i) * pitch * 2 + (u - i * units * 2)] = make_uint4(0u, 0u, 0u, 0u);
+  }
 }
 
 // The bf16 attention's scheme (see attn_tcgen05.cuh: the same warps, tiles, halves and order of MMAs, two CTAs an SM) with lengths that are
@@ -599,7 +578,7 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
     range[0] = 2 * n_tiles;
     range[1] = len - t_begin * kBN;
   }
-  if (warp < 4 && norms != nullptr) {                    // the largest squared norm of this head's keys
+  if (warp < 4) {                    // the largest squared norm of this head's keys
     unsigned most = 0u;
     const int blocks = (q8_length(P.lens, seq, P.cap) + kWidenRows - 1) / kWidenRows;
     for (int b = threadIdx.x; b < blocks; b += 128) most = max(most, norms[((size_t)seq * (plane_rows / kWidenRows) + b) * P.HK + hk]);
@@ -712,9 +691,9 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
     float m = -INFINITY, l = 0.0f;
     bool ok = true;
     // Upper bound of this row's logits in log2 units, |q| |k|_max log2(e) / 8, for the fixed reference (see attn_tcgen05.cuh).
-    float bound = INFINITY;
+    float bound;
     bool fixed_ref = false, in_range = false;
-    if (norms != nullptr) {
+    {
       const float kmax2 = __uint_as_float(max(max(top[0], top[1]), max(top[2], top[3])));
       float qn2 = 0.0f;
 #pragma unroll
@@ -924,7 +903,7 @@ inline AttnQ8Plan attn_q8_plan(int seqs, int M, int H, int HK, int cap) {
   }
   A.o_part = A.parts == 1 ? 0 : (size_t)A.parts * A.seqs * M * H * kHD * 4;
   A.ml_part = A.parts == 1 ? 0 : (size_t)A.parts * A.seqs * M * H * 8;
-  A.bytes = A.planes + A.o_part + A.ml_part + (A.planes ? (size_t)A.seqs * (A.plane_rows / kWidenRows * (1 + (HK <= kWidenHeads ? HK : 0)) + 1) * 4 : 0);
+  A.bytes = A.planes + A.o_part + A.ml_part + (A.planes ? (size_t)A.seqs * (A.plane_rows / kWidenRows * (1 + HK) + 1) * 4 : 0);
   return A;
 }
 
@@ -948,7 +927,7 @@ static inline int attn_q8_launch(AttnQ8Args P, void* scratch, cudaStream_t st, i
       const int blocks = A.plane_rows / kWidenRows;
       int* first = reinterpret_cast<int*>(planes + A.planes + A.o_part + A.ml_part);
       int* counts = P.live ? first + (size_t)A.seqs * blocks : nullptr;
-      unsigned* norms = P.HK <= kWidenHeads ? reinterpret_cast<unsigned*>(first + (size_t)A.seqs * (blocks + 1)) : nullptr;
+      unsigned* norms = reinterpret_cast<unsigned*>(first + (size_t)A.seqs * (blocks + 1));
       const WidenArgs W = {reinterpret_cast<const uint4*>(P.kq), reinterpret_cast<const uint4*>(P.vq), P.kx, P.vx, P.lens, P.live, first, counts,
                            reinterpret_cast<uint4*>(planes), reinterpret_cast<uint4*>(planes + side), norms, P.cap, P.HK, A.plane_rows};
       CUtensorMap tk, tv;
@@ -961,7 +940,7 @@ static inline int attn_q8_launch(AttnQ8Args P, void* scratch, cudaStream_t st, i
         e = launch_dependent(k_live_rows, dim3(P.seqs), 1024, 1, 0, st, true, LiveArgs{P.lens, P.live, first, counts, P.cap, blocks});
         *launches += 1;
       }
-      if (e == cudaSuccess) e = launch_dependent(k_widen_q8, dim3(blocks, P.seqs, 2), 256, 1, 0, st, true, W);
+      if (e == cudaSuccess) e = launch_dependent(k_widen_q8, dim3(blocks, P.seqs, (P.HK + kWidenHeads - 1) / kWidenHeads * 2), 256, 1, 0, st, true, W);
       static std::atomic<uint64_t> smem_many;
       if (e == cudaSuccess) e = allow_smem(k_attn_q8_many, kManySmem, smem_many);
       if (e == cudaSuccess) e = launch_dependent(k_attn_q8_many, dim3((unsigned)ctas), kAttnThreads, 1, kManySmem, st, true, tk, tv, P, (const int*)counts, (const unsigned*)norms, A.plane_rows);
