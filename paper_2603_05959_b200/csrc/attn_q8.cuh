@@ -526,8 +526,8 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
   unsigned char* sK = sQ + kQBytes;
   unsigned char* sV = sK + kKVStages * kTileBytes;
   AttnBarriers* B = reinterpret_cast<AttnBarriers*>(smem + kManyBar);
-  unsigned* top = reinterpret_cast<unsigned*>(B + 1);    // [4]
-  volatile int* range = reinterpret_cast<volatile int*>(top + 4);             // halves of this CTA, live rows from its first tile on: read where they are needed
+  unsigned* top = reinterpret_cast<unsigned*>(B + 1);    // [8]
+  volatile int* range = reinterpret_cast<volatile int*>(top + 8);             // halves of this CTA, live rows from its first tile on: read where they are needed
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const Place at0(P, blockIdx.x);
   const int hk = at0.hk, part = at0.part, seq = at0.seq;
@@ -560,7 +560,16 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
   const int len = counts != nullptr ? counts[seq] : q8_length(P.lens, seq, P.cap);      // live rows
   const int tiles_total = (len + kBN - 1) / kBN;
   const int t_begin = (int)((long long)part * tiles_total / P.parts), n_tiles = (int)((long long)(part + 1) * tiles_total / P.parts) - t_begin;
-  {                                                      // Q: 128 rows x 8 groups of 8 columns, rows past the last zero
+  // What the first tiles need is requested at once: K and V by the producer's thread, the queries (128 rows x 8 groups of 8 columns, rows
+  // past the last zero) and the norms of this head's keys by all.
+  const int plane_row = seq * plane_rows + t_begin * kBN;
+  if (warp == 4 && lane == 0 && n_tiles > 0) {
+    mbar_expect_tx(&B->k_full[0], kTileBytes);
+    tma_load_2d(sK, &tm_k, hk * kHD, plane_row, &B->k_full[0]);
+    mbar_expect_tx(&B->v_full[0], kTileBytes);
+    tma_load_2d(sV, &tm_v, hk * kHD, plane_row, &B->v_full[0]);
+  }
+  {
     constexpr int kPer = kBM * 8 / kAttnThreads;
     uint4 x[kPer];
 #pragma unroll
@@ -568,22 +577,20 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
       const int idx = threadIdx.x + i * kAttnThreads, r = at0.row0 + (idx >> 3);
       x[i] = r < P.M * P.group ? *reinterpret_cast<const uint4*>(P.q + at0.q(P, r) + (idx & 7) * 8) : make_uint4(0u, 0u, 0u, 0u);
     }
+    unsigned most = 0u;
+    const int blocks = (q8_length(P.lens, seq, P.cap) + kWidenRows - 1) / kWidenRows;
+    for (int b = threadIdx.x; b < blocks; b += kAttnThreads) most = max(most, norms[((size_t)seq * (plane_rows / kWidenRows) + b) * P.HK + hk]);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int idx = threadIdx.x + i * kAttnThreads, r = idx >> 3;
       *reinterpret_cast<uint4*>(sQ + r * 128 + (((idx & 7) ^ (r & 7)) << 4)) = x[i];
     }
-  }
-  if (threadIdx.x == 0) {
-    range[0] = 2 * n_tiles;
-    range[1] = len - t_begin * kBN;
-  }
-  if (warp < 4) {                    // the largest squared norm of this head's keys
-    unsigned most = 0u;
-    const int blocks = (q8_length(P.lens, seq, P.cap) + kWidenRows - 1) / kWidenRows;
-    for (int b = threadIdx.x; b < blocks; b += 128) most = max(most, norms[((size_t)seq * (plane_rows / kWidenRows) + b) * P.HK + hk]);
     most = __reduce_max_sync(0xFFFFFFFFu, most);
     if (lane == 0) top[warp] = most;
+    if (threadIdx.x == 0) {
+      range[0] = 2 * n_tiles;
+      range[1] = len - t_begin * kBN;
+    }
   }
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   tc_fence_before();
@@ -596,10 +603,10 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
     if (warp == 4) {
       // ------------------------------------------------ TMA producer
       if (lane == 0) {
-        int issued_k = 0, issued_v = 0;
+        int issued_k = min(n_tiles, 1), issued_v = issued_k;                    // (the first tile's are under way)
         bool ok = true;
-        for (int it = 0; it < n_tiles && ok; ++it) {
-          const int s = it % kKVStages, row = seq * plane_rows + (t_begin + it) * kBN;
+        for (int it = 1; it < n_tiles && ok; ++it) {
+          const int s = it % kKVStages, row = plane_row + it * kBN;
           const uint32_t ph = (uint32_t)(it / kKVStages - 1) & 1u;
           if (it >= kKVStages) ok = mbar_wait(&B->k_empty[s], ph, B, P.status);
           if (!ok) break;
@@ -694,7 +701,7 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
     float bound;
     bool fixed_ref = false, in_range = false;
     {
-      const float kmax2 = __uint_as_float(max(max(top[0], top[1]), max(top[2], top[3])));
+      const float kmax2 = __uint_as_float(max(max(max(top[0], top[1]), max(top[2], top[3])), max(max(top[4], top[5]), max(top[6], top[7]))));
       float qn2 = 0.0f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -710,7 +717,7 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
       bound = sqrtf(qn2 * kmax2) * c;
     }
     for (int idx = 0; idx < range[0] && ok; ++idx) {    // idx = 2 * tile + half
-      const int it = idx >> 1, hf = idx & 1;
+      const int it = idx >> 1, hf = idx & 1, left = range[1] - idx * kHalf;
       // (every wait result is made warp-uniform before the warp meets an .aligned tensor-memory instruction)
       ok = __all_sync(0xFFFFFFFFu, mbar_wait(&B->s_full[hf], (uint32_t)it & 1u, B, P.status)) != 0;
       if (!ok) break;
@@ -720,7 +727,6 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
 #pragma unroll
         for (int j = 0; j < kHalf / 32; ++j) tmem_ld32(t_row + kColS + hf * kHalf + j * 32, s + j * 32);
         tmem_wait_ld();
-        const int left = range[1] - idx * kHalf;
         if (left < kHalf) {
 #pragma unroll
           for (int j = 0; j < kHalf; ++j)
@@ -769,7 +775,7 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
         in_range = fixed_ref && __all_sync(0xFFFFFFFFu, bound + m <= -1.0f - kPolyLowest) != 0;
         add = exp_pass(std::false_type{}, std::true_type{}, raw);
       } else if (fixed_ref) {
-        add = in_range && (idx + 1) * kHalf <= range[1] ? exp_pass(std::false_type{}, std::false_type{}, raw) : exp_pass(std::false_type{}, std::true_type{}, raw);
+        add = in_range && left >= kHalf ? exp_pass(std::false_type{}, std::false_type{}, raw) : exp_pass(std::false_type{}, std::true_type{}, raw);
       } else {
         add = exp_pass(std::true_type{}, std::true_type{}, raw);
         const float mx = raw * c;
@@ -841,19 +847,33 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
       unsigned block = blockIdx.x;
       asm volatile("" : "+r"(block));                    // (taken apart again: nothing of it is kept through the loop)
       const Place at1(P, block);
-      const int rows = P.M * P.group, row0 = at1.row0;
-      const size_t shift = (size_t)at1.part * P.seqs * P.M * P.H * kHD;
-      const int words = one ? 8 : 16;                    // 16-byte words of a row
-#pragma unroll 4
-      for (int u = lane; u < 32 * words; u += 32) {
-        const int r = u / words, w = u - r * words, at_row = row0 + warp * 32 + r;
-        if (at_row < rows) {
-          const uint4 x = *reinterpret_cast<const uint4*>(stage + r * kOutRow + w * 16);
-          if (one) *reinterpret_cast<uint4*>(P.out + at1.q(P, at_row) + w * 8) = x;
-          else *reinterpret_cast<uint4*>(P.o_part + shift + at1.q(P, at_row) + w * 4) = x;
+      // (a lane's row of the result, in rows of a head; -1 past the last)
+      const int mine = at1.row0 + row < P.M * P.group ? (int)(at1.q(P, at1.row0 + row) / kHD) : -1;
+      const size_t shift = (size_t)at1.part * P.seqs * P.M * P.H;
+      auto store = [&](auto lanes, unsigned char* to) {  // lanes: 16-byte words of a row
+        constexpr int kLanes = decltype(lanes)::value;
+        const int sub = lane % kLanes, r0 = lane / kLanes;
+        const unsigned char* from = stage + r0 * kOutRow + sub * 16;
+#pragma unroll
+        for (int i = 0; i < kLanes; i += 8) {
+          uint4 w[8];
+          int at[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            w[e] = *reinterpret_cast<const uint4*>(from + (i + e) * (32 / kLanes) * kOutRow);
+            at[e] = __shfl_sync(0xFFFFFFFFu, mine, r0 + (i + e) * (32 / kLanes));
+          }
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (at[e] >= 0) *reinterpret_cast<uint4*>(to + (size_t)at[e] * (kLanes * 16) + sub * 16) = w[e];
         }
+      };
+      if (one) {
+        store(std::integral_constant<int, 8>{}, reinterpret_cast<unsigned char*>(P.out));
+      } else {
+        store(std::integral_constant<int, 16>{}, reinterpret_cast<unsigned char*>(P.o_part + shift * kHD));
+        if (mine >= 0) P.ml_part[shift + mine] = seen ? make_float2(fmaxf(m, kDeadMax), l) : make_float2(kDeadMax, kDeadSum);
       }
-      if (!one && row0 + row < rows) P.ml_part[(shift + at1.q(P, row0 + row)) / kHD] = seen ? make_float2(fmaxf(m, kDeadMax), l) : make_float2(kDeadMax, kDeadSum);
     }
   }
 
