@@ -36,9 +36,8 @@ __device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b) {
   const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
   return *reinterpret_cast<const uint32_t*>(&d);
 }
-// Two int8, in the low bytes of the halves of x, as a pair of bf16, exact: 128 + the low seven bits, less 128 or, of a negative one, 256.
-// (x: the bytes in halves whose high bytes are 0x43)
-__device__ __forceinline__ uint32_t int8_to_bf16x2(uint32_t x) { return sub_bf16x2(x & 0xFF7FFF7Fu, x & 0xFF80FF80u); }
+// Two int8, the low bytes of the halves of x, as a pair of bf16, exact: 128 + the low seven bits, less 128 or, of a negative one, 256.
+__device__ __forceinline__ uint32_t int8_to_bf16x2(uint32_t x) { return sub_bf16x2((x & 0x007F007Fu) | 0x43004300u, (x & 0x00800080u) | 0x43004300u); }
 
 // ---------------------------------------------------------------- few rows: the cache streams through, once per 8, 16 or 32 rows
 //
@@ -52,14 +51,18 @@ __device__ __forceinline__ uint32_t int8_to_bf16x2(uint32_t x) { return sub_bf16
 //           the sum of two bf16 numbers, the halves of the operand again; otherwise it is rounded to one (2^-9).
 // Which cached row or column an operand's row or column stands for is free, so each lane takes 16 bytes of a K row and 8
 // bytes of a V row at once.
-constexpr int kFewWarps = 8, kFewStages = 3, kFewKeys = 32;
+// A CTA has an SM to itself: of 8 or 16 rows sixteen warps, of 32, whose registers leave no more, eight.
+__host__ __device__ constexpr int few_warps(int rows) { return rows == 32 ? 8 : 16; }
+constexpr int kFewStages = 3, kFewKeys = 32;
 constexpr int kFewX = 2 * kFewKeys * 64;                 // of a stage: K, V, then the exponents of K and V and the mask, 32 bytes each
 constexpr int kFewStage = kFewX + 128;
-__host__ __device__ constexpr int few_smem_bytes() { return kFewWarps * kFewStages * kFewStage; }
+constexpr int kFewTable = kFewKeys * 16;                 // of a warp: (step of K, 0 or -inf under the mask, step of V) for each row of its tile
+__host__ __device__ constexpr int few_smem_bytes(int rows) { return few_warps(rows) * (kFewStages * kFewStage + kFewTable); }
 static_assert(kFewStages * kFewStage >= 32 * (64 + 2) * 4, "a warp's result does not fit its stages");
 
 template <int ROWS>
-__global__ void __launch_bounds__(kFewWarps * 32) k_attn_q8_few(const AttnQ8Args P) {
+__global__ void __launch_bounds__(few_warps(ROWS) * 32, 1) k_attn_q8_few(const AttnQ8Args P) {
+  constexpr int kFewWarps = few_warps(ROWS);
   constexpr bool PACK = ROWS == 8;
   constexpr int T = PACK ? 1 : ROWS / 16;                // operands of 16 rows
   constexpr int R = PACK ? 1 : 2;                        // rows of an operand a thread holds scores of
@@ -77,9 +80,50 @@ __global__ void __launch_bounds__(kFewWarps * 32) k_attn_q8_few(const AttnQ8Args
     return (((size_t)seq * P.M + m) * P.H + (size_t)hk * P.group + (r - m * P.group)) * 64;
   };
 
+  // ---- the cache, tile by tile
+  unsigned char* stages = smem + warp * kFewStages * kFewStage;
+  const size_t pitch = (size_t)P.HK * 64, base = ((size_t)seq * P.cap * P.HK + hk) * 64, xbase = ((size_t)seq * P.HK + hk) * P.cap;
+  const int first = part * kFewWarps + warp, stride = P.parts * kFewWarps;
+  float4* table = reinterpret_cast<float4*>(smem + kFewWarps * kFewStages * kFewStage + warp * kFewTable);
+  const int8_t* k_lane = P.kq + base + (size_t)g * pitch + t * 16;            // this lane's part of the cache's first row and every eighth after it
+  const int8_t* v_lane = P.vq + base + (size_t)g * pitch + t * 16;
+  // K rows lie so that the two of a lane's adjacent scores are four apart; V rows 2 and 3 of four have their halves exchanged.
+  const int k_to = ((g & 3) * 2 + (g >> 2)) * 64 + t * 16, v_to = 2048 + g * 64 + (t ^ (g & 2)) * 16;
+  const uint8_t* x_lane = nullptr;                       // lanes 0 to 5: sixteen bytes of the exponents and the mask
+  if (lane < 4 || (lane < 6 && P.live != nullptr))
+    x_lane = (lane < 2 ? P.kx + xbase : (lane < 4 ? P.vx + xbase : P.live + (size_t)seq * P.cap)) + (lane & 1) * 16;
+  auto request = [&](int tile, int stage) {
+    if (tile < tiles) {
+      unsigned char* s = stages + stage * kFewStage;
+      const int row0 = tile * kFewKeys;
+      const size_t at = (size_t)row0 * pitch;
+      if (row0 + kFewKeys <= len) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          copy16(s + k_to + i * 512, k_lane + at + i * 8 * pitch, true);
+          copy16(s + v_to + i * 512, v_lane + at + i * 8 * pitch, true);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const bool in = row0 + 8 * i + g < len;
+          const size_t from = in ? at + i * 8 * pitch : 0;
+          copy16(s + k_to + i * 512, in ? k_lane + from : P.kq, in);
+          copy16(s + v_to + i * 512, in ? v_lane + from : P.vq, in);
+        }
+      }
+      // (the capacity is a multiple of 16)
+      if (x_lane != nullptr && row0 + (lane & 1) * 16 < P.cap) copy16(s + kFewX + lane * 16, x_lane + row0, true);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int s = 0; s < kFewStages - 1; ++s) request(first + s * stride, s);
+
   // ---- the operands of Q: [tile][0: hi (or hi and lo), 1: lo][32 columns][register]
   uint32_t qa[T][PACK ? 1 : 2][2][4];
   float f[T][R];                                         // a score in log2 units is f x the whole numbers' product x 2^(kx - 127)
+  bool odd[T][R];                                        // a query that is not finite: its result is not a number
 #pragma unroll
   for (int i = 0; i < T; ++i)
 #pragma unroll
@@ -102,7 +146,8 @@ __global__ void __launch_bounds__(kFewWarps * 32) k_attn_q8_few(const AttnQ8Args
       const bool finite = most < 0x7F800000u, some = finite && most >= 0x00800000u;
       const float u0 = some ? __int_as_float((up / 2 + 127) << 23) : 0.0f, u1 = some ? __int_as_float((up - up / 2 + 127) << 23) : 0.0f;
       // log2(e) / 8 2^(e - 13) 2^-6: cached values are 2^(x - 133)
-      f[i][half] = some ? ldexpf(1.4426950408889634f * 0.125f, e2 - 19) : (finite ? 0.0f : __int_as_float(0x7FC00000));
+      f[i][half] = some ? ldexpf(1.4426950408889634f * 0.125f, e2 - 19) : 0.0f;
+      odd[i][half] = !finite;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         int hi[4], lo[4];
@@ -125,29 +170,6 @@ __global__ void __launch_bounds__(kFewWarps * 32) k_attn_q8_few(const AttnQ8Args
       }
     }
 
-  // ---- the cache, tile by tile
-  unsigned char* stages = smem + warp * kFewStages * kFewStage;
-  const size_t pitch = (size_t)P.HK * 64, base = ((size_t)seq * P.cap * P.HK + hk) * 64, xbase = ((size_t)seq * P.HK + hk) * P.cap;
-  const int first = part * kFewWarps + warp, stride = P.parts * kFewWarps;
-  auto request = [&](int tile, int stage) {
-    if (tile < tiles) {
-      unsigned char* s = stages + stage * kFewStage;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int key = 8 * i + g, row = tile * kFewKeys + key, from = min(row, len - 1);
-        const bool in = row < len;
-        // K rows lie so that the two of a lane's adjacent scores are four apart; V rows 2 and 3 of four have their halves exchanged
-        copy16(s + ((key & ~7) + (key & 3) * 2 + (key >> 2 & 1)) * 64 + t * 16, P.kq + base + (size_t)from * pitch + t * 16, in);
-        copy16(s + 2048 + key * 64 + (t ^ (key & 2)) * 16, P.vq + base + (size_t)from * pitch + t * 16, in);
-      }
-      if (lane < 6 && (lane < 4 || P.live != nullptr)) {
-        const int which = lane >> 1, row = tile * kFewKeys + (lane & 1) * 16;
-        const uint8_t* src = which == 0 ? P.kx + xbase : (which == 1 ? P.vx + xbase : P.live + (size_t)seq * P.cap);
-        copy16(s + kFewX + lane * 16, src + min(row, P.cap - 16), row < P.cap);
-      }
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
   float m[T][R], l[T][R], o[T][8][4];
 #pragma unroll
   for (int i = 0; i < T; ++i) {
@@ -156,8 +178,6 @@ __global__ void __launch_bounds__(kFewWarps * 32) k_attn_q8_few(const AttnQ8Args
 #pragma unroll
     for (int d = 0; d < 8; ++d) o[i][d][0] = o[i][d][1] = o[i][d][2] = o[i][d][3] = 0.0f;
   }
-#pragma unroll
-  for (int s = 0; s < kFewStages - 1; ++s) request(first + s * stride, s);
   int stage = 0;
 #pragma unroll 1
   for (int tile = first; tile < tiles; tile += stride) {
@@ -167,36 +187,38 @@ __global__ void __launch_bounds__(kFewWarps * 32) k_attn_q8_few(const AttnQ8Args
     const unsigned char* s = stages + stage * kFewStage;
     stage = stage + 1 == kFewStages ? 0 : stage + 1;
 
+    {                                                    // a lane a row: what its scores and its weight are multiplied with
+      const bool in = tile * kFewKeys + lane < len && (P.live == nullptr || s[kFewX + 64 + lane] != 0);
+      // (255: infinity, which a block of zeros makes NaN)
+      table[lane] = in ? make_float4(__int_as_float((int)s[kFewX + lane] << 23), 0.0f, q8_step(s[kFewX + 32 + lane]), 0.0f) : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
+    }
+    __syncwarp();
     float sc[T][R][8], vs[8];                            // scores of keys 8 b + t (even entries) and 8 b + t + 4
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
       const uint4 kw = *reinterpret_cast<const uint4*>(s + (8 * b + g) * 64 + t * 16);
-      float ks[2];
-      bool in[2];
+      float4 x[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const int key = 8 * b + t + 4 * e;
-        in[e] = tile * kFewKeys + key < len && (P.live == nullptr || s[kFewX + 64 + key] != 0);
-        ks[e] = __int_as_float((int)s[kFewX + key] << 23);     // (255: infinity, which a block of zeros makes NaN)
-        vs[2 * b + e] = in[e] ? q8_step(s[kFewX + 32 + key]) : 0.0f;
+        x[e] = table[8 * b + t + 4 * e];
+        vs[2 * b + e] = x[e].z;
       }
 #pragma unroll
       for (int i = 0; i < T; ++i) {
-        int c[4] = {0, 0, 0, 0};
-        mma_s8(c, qa[i][0][0][0], qa[i][0][0][1], qa[i][0][0][2], qa[i][0][0][3], kw.x, kw.y);
+        int c[4];
+        mma_s8_first(c, qa[i][0][0][0], qa[i][0][0][1], qa[i][0][0][2], qa[i][0][0][3], kw.x, kw.y);
         mma_s8(c, qa[i][0][1][0], qa[i][0][1][1], qa[i][0][1][2], qa[i][0][1][3], kw.z, kw.w);
         if constexpr (PACK) {
 #pragma unroll
-          for (int e = 0; e < 2; ++e) sc[i][0][2 * b + e] = in[e] ? (float)(c[e] * 256 + c[e + 2]) * (f[i][0] * ks[e]) : -INFINITY;
+          for (int e = 0; e < 2; ++e) sc[i][0][2 * b + e] = fmaf((float)(c[e] * 256 + c[e + 2]), f[i][0] * x[e].x, x[e].y);
         } else {
-          int d[4] = {0, 0, 0, 0};
-          mma_s8(d, qa[i][1][0][0], qa[i][1][0][1], qa[i][1][0][2], qa[i][1][0][3], kw.x, kw.y);
+          int d[4];
+          mma_s8_first(d, qa[i][1][0][0], qa[i][1][0][1], qa[i][1][0][2], qa[i][1][0][3], kw.x, kw.y);
           mma_s8(d, qa[i][1][1][0], qa[i][1][1][1], qa[i][1][1][2], qa[i][1][1][3], kw.z, kw.w);
 #pragma unroll
           for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-              sc[i][r][2 * b + e] = in[e] ? (float)(c[2 * r + e] * 256 + d[2 * r + e]) * (f[i][r] * ks[e]) : -INFINITY;
+            for (int e = 0; e < 2; ++e) sc[i][r][2 * b + e] = fmaf((float)(c[2 * r + e] * 256 + d[2 * r + e]), f[i][r] * x[e].x, x[e].y);
         }
       }
     }
@@ -263,13 +285,12 @@ __global__ void __launch_bounds__(kFewWarps * 32) k_attn_q8_few(const AttnQ8Args
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const uint32_t x = half ? v[2 * e].y : v[2 * e].x, y = half ? v[2 * e + 1].y : v[2 * e + 1].x;
-          w[e][0] = __byte_perm(x, y, 0x5140);
-          w[e][1] = __byte_perm(x, y, 0x7362);
+          w[e][0] = __byte_perm(x, y, 0x5410);           // columns 0 and 1 of both, then 2 and 3
+          w[e][1] = __byte_perm(x, y, 0x7632);
         }
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
-          const int sel = d & 1 ? 0x4342 : 0x4140;       // (byte 4: 0x43)
-          const uint32_t b0 = int8_to_bf16x2(__byte_perm(w[0][d >> 1], 0x43434343u, sel)), b1 = int8_to_bf16x2(__byte_perm(w[1][d >> 1], 0x43434343u, sel));
+          const uint32_t b0 = int8_to_bf16x2(w[0][d >> 1] >> (d & 1) * 8), b1 = int8_to_bf16x2(w[1][d >> 1] >> (d & 1) * 8);
 #pragma unroll
           for (int i = 0; i < T; ++i) mma_bf16(o[i][4 * half + d], pa[i][b][0], pa[i][b][1], pa[i][b][2], pa[i][b][3], b0, b1);
         }
@@ -288,6 +309,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) k_attn_q8_few(const AttnQ8Args
       float x = l[i][r];
       x += __shfl_xor_sync(0xFFFFFFFFu, x, 1);
       x += __shfl_xor_sync(0xFFFFFFFFu, x, 2);
+      if (odd[i][r] && m[i][r] != -INFINITY) x = __int_as_float(0x7FC00000);
       const int row = 16 * i + 8 * r + g;
       if (t == 0) mine[ROWS * 64 + row] = m[i][r], mine[ROWS * 65 + row] = x;
 #pragma unroll
@@ -463,8 +485,8 @@ __global__ void __launch_bounds__(256) k_widen_q8(const WidenArgs P) {
       uint32_t o[8];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        o[2 * e] = mul_bf16x2(int8_to_bf16x2(__byte_perm(in[e], 0x43434343u, 0x4140)), step);
-        o[2 * e + 1] = mul_bf16x2(int8_to_bf16x2(__byte_perm(in[e], 0x43434343u, 0x4342)), step);
+        o[2 * e] = mul_bf16x2(int8_to_bf16x2(__byte_perm(in[e], 0u, 0x4140)), step);
+        o[2 * e + 1] = mul_bf16x2(int8_to_bf16x2(__byte_perm(in[e], 0u, 0x4342)), step);
       }
       uint4* d = dst + (size_t)(to + i) * pitch * 2 + 2 * part;
       d[0] = make_uint4(o[0], o[1], o[2], o[3]);
@@ -917,8 +939,8 @@ inline AttnQ8Plan attn_q8_plan(int seqs, int M, int H, int HK, int cap) {
     A.tile = rows <= 8 ? 8 : (rows <= 16 ? 16 : 32);
     A.seqs = seqs;
     A.q_tiles = (int)((rows + A.tile - 1) / A.tile);
-    // as many CTAs as fit at once, while each warp has two tiles to take
-    const long long jobs = (long long)seqs * HK * A.q_tiles, places = 2 * 148, most = cap / (2 * kFewWarps * kFewKeys);
+    // as many CTAs as there are SMs, while each warp has a tile to take
+    const long long jobs = (long long)seqs * HK * A.q_tiles, places = 148, most = cap / (few_warps(A.tile) * kFewKeys);
     A.parts = (int)std::max(1ll, std::min({(long long)kMaxSplits, places / jobs, most}));
   }
   A.o_part = A.parts == 1 ? 0 : (size_t)A.parts * A.seqs * M * H * kHD * 4;
@@ -968,8 +990,8 @@ static inline int attn_q8_launch(AttnQ8Args P, void* scratch, cudaStream_t st, i
     } else {
       const auto kernel = A.tile == 8 ? k_attn_q8_few<8> : (A.tile == 16 ? k_attn_q8_few<16> : k_attn_q8_few<32>);
       static std::atomic<uint64_t> smem_few[3];
-      e = allow_smem(kernel, few_smem_bytes(), smem_few[A.tile == 8 ? 0 : (A.tile == 16 ? 1 : 2)]);
-      if (e == cudaSuccess) e = launch_dependent(kernel, dim3((unsigned)ctas), kFewWarps * 32, 1, few_smem_bytes(), st, true, P);
+      e = allow_smem(kernel, few_smem_bytes(A.tile), smem_few[A.tile == 8 ? 0 : (A.tile == 16 ? 1 : 2)]);
+      if (e == cudaSuccess) e = launch_dependent(kernel, dim3((unsigned)ctas), few_warps(A.tile) * 32, 1, few_smem_bytes(A.tile), st, true, P);
       *launches += 1;
     }
     if (e != cudaSuccess) { g_attn_last_error = (int)e; return OVGGT_ERR_CUDA; }
