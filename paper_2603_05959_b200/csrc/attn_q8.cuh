@@ -28,6 +28,19 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_u8s8(int (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Byte c of each of four words, in order, in word c.
+__device__ __forceinline__ void transpose4(uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t (&o)[4]) {
+  const uint32_t ab = __byte_perm(a, b, 0x5140), cd = __byte_perm(c, d, 0x5140), ab2 = __byte_perm(a, b, 0x7362), cd2 = __byte_perm(c, d, 0x7362);
+  o[0] = __byte_perm(ab, cd, 0x5410);
+  o[1] = __byte_perm(ab, cd, 0x7632);
+  o[2] = __byte_perm(ab2, cd2, 0x5410);
+  o[3] = __byte_perm(ab2, cd2, 0x7632);
+}
 // 16 bytes into shared memory behind the thread's back; zeros where `in` is false.
 __device__ __forceinline__ void copy16(void* dst, const void* src, bool in) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(in ? 16 : 0) : "memory");
@@ -47,17 +60,21 @@ __device__ __forceinline__ uint32_t int8_to_bf16x2(uint32_t x) { return sub_bf16
 //   scores  by int8 MMAs on the cached bytes as they are.  A row of Q is taken as whole numbers of 15 bits, q = 2^(e - 13) (256 hi + lo), two int8
 //           operands: exact for elements down to 2^-6 of the row's largest, to 2^-14 of it for the rest.  With at
 //           most 8 rows hi and lo are the two halves of one operand of 16 rows.
-//   P V     by bf16 MMAs: the cached bytes are exact in bf16, their row's power of two goes into P.  With at most 8 rows P is
-//           the sum of two bf16 numbers, the halves of the operand again; otherwise it is rounded to one (2^-9).
+//   P V     with at most 8 rows by int8 MMAs too: a weight p 2^(x - 133) as a whole number of 31 bits, 2^-23 of a reference that follows the largest
+//           weight, four unsigned bytes in the halves of two operands; the cached bytes of four rows are only put side by side.  The int32 sums
+//           are exact and go into fp32 when the reference moves.  With more rows, where that many sums do not fit the registers, by bf16 MMAs: the
+//           cached bytes are exact in bf16, a weight is rounded to it (2^-8).  (One row over 32768, 16 heads: 17 us, by bf16 MMAs 22.)
 // Which cached row or column an operand's row or column stands for is free, so each lane takes 16 bytes of a K row and 8
 // bytes of a V row at once.
-// A CTA has an SM to itself: of 8 or 16 rows sixteen warps, of 32, whose registers leave no more, eight.
-__host__ __device__ constexpr int few_warps(int rows) { return rows == 32 ? 8 : 16; }
+// A CTA has an SM to itself, and as many warps as its registers leave (8 rows by 16 warps, which spill: 28 us where 12 take 25, four tokens over 16384 rows).
+__host__ __device__ constexpr int few_warps(int rows) { return rows == 8 ? 12 : (rows == 16 ? 16 : 8); }
 constexpr int kFewStages = 3, kFewKeys = 32;
 constexpr int kFewX = 2 * kFewKeys * 64;                 // of a stage: K, V, then the exponents of K and V and the mask, 32 bytes each
 constexpr int kFewStage = kFewX + 128;
 constexpr int kFewTable = kFewKeys * 16;                 // of a warp: (step of K, 0 or -inf under the mask, step of V) for each row of its tile
-__host__ __device__ constexpr int few_smem_bytes(int rows) { return few_warps(rows) * (kFewStages * kFewStage + kFewTable); }
+__host__ __device__ constexpr int few_smem_bytes(int rows) {
+  return few_warps(rows) * (kFewStages * kFewStage + kFewTable) + (rows == 8 ? 1 : rows / 8) * 1024 + rows * 8;
+}
 static_assert(kFewStages * kFewStage >= 32 * (64 + 2) * 4, "a warp's result does not fit its stages");
 
 template <int ROWS>
@@ -120,57 +137,89 @@ __global__ void __launch_bounds__(few_warps(ROWS) * 32, 1) k_attn_q8_few(const A
 #pragma unroll
   for (int s = 0; s < kFewStages - 1; ++s) request(first + s * stride, s);
 
-  // ---- the operands of Q: [tile][0: hi (or hi and lo), 1: lo][32 columns][register]
-  uint32_t qa[T][PACK ? 1 : 2][2][4];
+  // ---- the operands of Q, eight rows a warp, by way of shared memory: [tile][0: hi (or hi and lo), 1: lo][32 columns][register]
+  constexpr int L = PACK ? 1 : 2;
+  uint4* q_sh = reinterpret_cast<uint4*>(smem + kFewWarps * (kFewStages * kFewStage + kFewTable));      // [T][L][2][lane]
+  float2* f_sh = reinterpret_cast<float2*>(q_sh + T * L * 2 * 32);                                        // [ROWS]
+  if (warp < T * R) {
+    const int i = warp / R, half = warp % R, r = row0 + 16 * i + 8 * half + g;
+    float x[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = 0.0f;
+    if (r < rows) {
+      const uint4* p = reinterpret_cast<const uint4*>(P.q + q_at(r) + 16 * t);
+      unpack<kBF16>(p[0], x);
+      unpack<kBF16>(p[1], x + 8);
+    }
+    uint32_t most = 0;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) most = max(most, __float_as_uint(x[e]) & 0x7FFFFFFFu);
+    most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
+    most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
+    const int e2 = (int)(most >> 23) - 127, up = 13 - e2;
+    const bool finite = most < 0x7F800000u, some = finite && most >= 0x00800000u;
+    const float u0 = some ? __int_as_float((up / 2 + 127) << 23) : 0.0f, u1 = some ? __int_as_float((up - up / 2 + 127) << 23) : 0.0f;
+    // log2(e) / 8 2^(e - 13) 2^-6: cached values are 2^(x - 133)
+    if (t == 0) f_sh[16 * i + 8 * half + g] = make_float2(some ? ldexpf(1.4426950408889634f * 0.125f, e2 - 19) : 0.0f, finite ? 0.0f : 1.0f);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      int hi[4], lo[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int z = some ? __float2int_rn(x[4 * w + e] * u0 * u1) : 0;
+        hi[e] = (z + 128) >> 8;
+        lo[e] = z - hi[e] * 256;
+      }
+      const uint32_t ph = (hi[0] & 255) | (hi[1] & 255) << 8 | (hi[2] & 255) << 16 | (uint32_t)hi[3] << 24;
+      const uint32_t pl = (lo[0] & 255) | (lo[1] & 255) << 8 | (lo[2] & 255) << 16 | (uint32_t)lo[3] << 24;
+      // word w: columns 16 t + 4 w on: k-step w / 2, its first or second half; register of the operand: + 1 for rows 8 to 15
+      uint32_t* at = reinterpret_cast<uint32_t*>(q_sh + ((i * L) * 2 + (w >> 1)) * 32 + lane) + (w & 1) * 2;
+      if constexpr (PACK) {
+        at[0] = ph;
+        at[1] = pl;
+      } else {
+        at[half] = ph;
+        at[2 * 32 * 4 + half] = pl;
+      }
+    }
+  }
+  __syncthreads();
+  uint32_t qa[T][L][2][4];
   float f[T][R];                                         // a score in log2 units is f x the whole numbers' product x 2^(kx - 127)
   bool odd[T][R];                                        // a query that is not finite: its result is not a number
 #pragma unroll
-  for (int i = 0; i < T; ++i)
+  for (int i = 0; i < T; ++i) {
 #pragma unroll
-    for (int half = 0; half < R; ++half) {
-      const int r = row0 + 16 * i + 8 * half + g;
-      float x[16];
+    for (int p = 0; p < 2 * L; ++p) *reinterpret_cast<uint4*>(qa[i][p >> 1][p & 1]) = q_sh[(i * 2 * L + p) * 32 + lane];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] = 0.0f;
-      if (r < rows) {
-        const uint4* p = reinterpret_cast<const uint4*>(P.q + q_at(r) + 16 * t);
-        unpack<kBF16>(p[0], x);
-        unpack<kBF16>(p[1], x + 8);
-      }
-      uint32_t most = 0;
+    for (int r = 0; r < R; ++r) {
+      const float2 x = f_sh[16 * i + 8 * r + g];
+      f[i][r] = x.x;
+      odd[i][r] = x.y != 0.0f;
+    }
+  }
+
+  float m[T][R], l[T][R], o[T][8][4];                    // O: with at most 8 rows two columns a register pair, [0] and [1]
+  int c1[PACK ? 8 : 1][4], c2[PACK ? 8 : 1][4], since = 0;   // what the int8 MMAs have summed up since O was last brought up to date, in how many tiles
+  float mv = -INFINITY;                                  // log2 of the reference weight
 #pragma unroll
-      for (int e = 0; e < 16; ++e) most = max(most, __float_as_uint(x[e]) & 0x7FFFFFFFu);
-      most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
-      most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
-      const int e2 = (int)(most >> 23) - 127, up = 13 - e2;
-      const bool finite = most < 0x7F800000u, some = finite && most >= 0x00800000u;
-      const float u0 = some ? __int_as_float((up / 2 + 127) << 23) : 0.0f, u1 = some ? __int_as_float((up - up / 2 + 127) << 23) : 0.0f;
-      // log2(e) / 8 2^(e - 13) 2^-6: cached values are 2^(x - 133)
-      f[i][half] = some ? ldexpf(1.4426950408889634f * 0.125f, e2 - 19) : 0.0f;
-      odd[i][half] = !finite;
+  for (int d = 0; d < (PACK ? 8 : 1); ++d)
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        int hi[4], lo[4];
+    for (int e = 0; e < 4; ++e) c1[d][e] = c2[d][e] = 0;
+  auto take_sums = [&](float scale) {                    // O = (O + sums) scale
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int z = some ? __float2int_rn(x[4 * w + e] * u0 * u1) : 0;
-          hi[e] = (z + 128) >> 8;
-          lo[e] = z - hi[e] * 256;
-        }
-        const uint32_t ph = (hi[0] & 255) | (hi[1] & 255) << 8 | (hi[2] & 255) << 16 | (uint32_t)hi[3] << 24;
-        const uint32_t pl = (lo[0] & 255) | (lo[1] & 255) << 8 | (lo[2] & 255) << 16 | (uint32_t)lo[3] << 24;
-        // word w: columns 16 t + 4 w on: k-step w / 2, its first or second half; register of the operand: + 1 for rows 8 to 15
-        if constexpr (PACK) {
-          qa[i][0][w >> 1][(w & 1) * 2] = ph;
-          qa[i][0][w >> 1][(w & 1) * 2 + 1] = pl;
-        } else {
-          qa[i][0][w >> 1][(w & 1) * 2 + half] = ph;
-          qa[i][1][w >> 1][(w & 1) * 2 + half] = pl;
-        }
+    for (int d = 0; d < (PACK ? 8 : 1); ++d) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float hi = fmaf((float)c1[d][e], 256.0f, (float)c1[d][e + 2]), lo = fmaf((float)c2[d][e], 256.0f, (float)c2[d][e + 2]);
+        o[0][d][e] = (o[0][d][e] + fmaf(hi, 65536.0f, lo)) * scale;
+        c1[d][e] = c1[d][e + 2] = c2[d][e] = c2[d][e + 2] = 0;
       }
     }
-
-  float m[T][R], l[T][R], o[T][8][4];
+    since = 0;
+  };
+  constexpr float kUnits = 23.0f, kRoom = 8.0f;          // a reference weight is 2^23 units; another is at most 2^8 of it
+  constexpr int kSumsMost = 2000;                        // tiles: 64000 x 255 x 127 is below 2^31
 #pragma unroll
   for (int i = 0; i < T; ++i) {
 #pragma unroll
@@ -190,7 +239,12 @@ __global__ void __launch_bounds__(few_warps(ROWS) * 32, 1) k_attn_q8_few(const A
     {                                                    // a lane a row: what its scores and its weight are multiplied with
       const bool in = tile * kFewKeys + lane < len && (P.live == nullptr || s[kFewX + 64 + lane] != 0);
       // (255: infinity, which a block of zeros makes NaN)
-      table[lane] = in ? make_float4(__int_as_float((int)s[kFewX + lane] << 23), 0.0f, q8_step(s[kFewX + 32 + lane]), 0.0f) : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
+      const uint32_t vx = s[kFewX + 32 + lane];
+      const float ks = __int_as_float((int)s[kFewX + lane] << 23);
+      if constexpr (PACK)                                // (the exponent of the value's step; a value that is not finite takes its score with it)
+        table[lane] = in ? make_float4(ks, vx == 255u ? __int_as_float(0x7FC00000) : 0.0f, (float)((int)vx - 133), 0.0f) : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
+      else
+        table[lane] = in ? make_float4(ks, 0.0f, q8_step(vx), 0.0f) : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
     }
     __syncwarp();
     float sc[T][R][8], vs[8];                            // scores of keys 8 b + t (even entries) and 8 b + t + 4
@@ -236,7 +290,20 @@ __global__ void __launch_bounds__(few_warps(ROWS) * 32, 1) k_attn_q8_few(const A
         top[i][r] = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 2));
         grown |= top[i][r] > m[i][r] + kRescaleThreshold;
       }
+    float topv = -INFINITY;
+    if constexpr (PACK) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) topv = fmaxf(topv, sc[0][0][e] + vs[e]);
+      topv = fmaxf(topv, __shfl_xor_sync(0xFFFFFFFFu, topv, 1));
+      topv = fmaxf(topv, __shfl_xor_sync(0xFFFFFFFFu, topv, 2));
+      grown |= topv > mv + kRoom || since >= kSumsMost;
+    }
     if (__any_sync(0xFFFFFFFFu, grown)) {
+      if constexpr (PACK) {
+        const float mn = fmaxf(mv, topv);
+        if (since > 0) take_sums(mv == mn ? 1.0f : ex2(mv - mn));
+        mv = mn;
+      }
 #pragma unroll
       for (int i = 0; i < T; ++i)
 #pragma unroll
@@ -244,55 +311,94 @@ __global__ void __launch_bounds__(few_warps(ROWS) * 32, 1) k_attn_q8_few(const A
           const float mn = fmaxf(m[i][r], top[i][r]), corr = m[i][r] == mn ? 1.0f : ex2(m[i][r] - mn);
           m[i][r] = mn;
           l[i][r] *= corr;
+          if constexpr (!PACK) {
 #pragma unroll
-          for (int d = 0; d < 8; ++d)
-            if constexpr (PACK) {
-#pragma unroll
-              for (int e = 0; e < 4; ++e) o[i][d][e] *= corr;
-            } else {
+            for (int d = 0; d < 8; ++d) {
               o[i][d][2 * r] *= corr;
               o[i][d][2 * r + 1] *= corr;
             }
+          }
         }
     }
-    uint32_t pa[T][2][4];                                // P of 16 keys as an operand
+    if constexpr (PACK) {
+      const float ref = m[0][0] == -INFINITY ? 0.0f : m[0][0], refv = mv == -INFINITY ? 0.0f : mv - kUnits;
+      const float2 back = make_float2(-ref, -ref), backv = make_float2(-refv, -refv);
+      float2 sum = make_float2(0.0f, 0.0f);
+      uint32_t w[8];
 #pragma unroll
-    for (int i = 0; i < T; ++i)
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        const float ref = m[i][r] == -INFINITY ? 0.0f : m[i][r];
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          const float p0 = ex2(sc[i][r][2 * b] - ref), p1 = ex2(sc[i][r][2 * b + 1] - ref);
-          l[i][r] += p0 + p1;
-          const float w0 = p0 * vs[2 * b], w1 = p1 * vs[2 * b + 1];
-          const uint32_t hi = pack_bf16(w0, w1);
-          pa[i][b >> 1][(b & 1) * 2 + r] = hi;
-          if constexpr (PACK) pa[i][b >> 1][(b & 1) * 2 + 1] = pack_bf16(w0 - __uint_as_float(hi << 16), w1 - __uint_as_float(hi & 0xFFFF0000u));
-        }
+      for (int b = 0; b < 4; ++b) {
+        const float2 x = make_float2(sc[0][0][2 * b], sc[0][0][2 * b + 1]), d = add2(x, back), y = add2(add2(x, make_float2(vs[2 * b], vs[2 * b + 1])), backv);
+        sum = add2(sum, make_float2(ex2(d.x), ex2(d.y)));
+        w[2 * b] = __float2uint_rn(ex2(y.x));
+        w[2 * b + 1] = __float2uint_rn(ex2(y.y));
       }
+      l[0][0] += sum.x + sum.y;
+      // operands: row g the top byte of the weights (a1) or the second lowest (a2), row g + 8 the byte below; 4 k's a register
+      uint32_t a1[4], a2[4], x[4];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {                        // 16 keys: 16 b + t, + 4, + 8, + 12
-      uint2 v[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int key = 16 * b + t + 4 * e;
-        v[e] = *reinterpret_cast<const uint2*>(s + 2048 + key * 64 + (((g >> 1) ^ (t & 2)) * 16) + (g & 1) * 8);
+      for (int h = 0; h < 2; ++h) {
+        transpose4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3], x);
+        a1[2 * h] = x[3];
+        a1[2 * h + 1] = x[2];
+        a2[2 * h] = x[1];
+        a2[2 * h + 1] = x[0];
       }
+      uint2 v[8];                                        // rows t, t + 4, ...: the order of the weights
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {             // four columns: pairs of keys side by side, then one column of both a register
-        uint32_t w[2][2];
+      for (int e = 0; e < 8; ++e) v[e] = *reinterpret_cast<const uint2*>(s + 2048 + (t + 4 * e) * 64 + (((g >> 1) ^ (t & 2)) * 16) + (g & 1) * 8);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const uint32_t x = half ? v[2 * e].y : v[2 * e].x, y = half ? v[2 * e + 1].y : v[2 * e + 1].x;
-          w[e][0] = __byte_perm(x, y, 0x5410);           // columns 0 and 1 of both, then 2 and 3
-          w[e][1] = __byte_perm(x, y, 0x7632);
-        }
+      for (int half = 0; half < 2; ++half) {             // four columns
+        uint32_t b0[4], b1[4];
+        transpose4(half ? v[0].y : v[0].x, half ? v[1].y : v[1].x, half ? v[2].y : v[2].x, half ? v[3].y : v[3].x, b0);
+        transpose4(half ? v[4].y : v[4].x, half ? v[5].y : v[5].x, half ? v[6].y : v[6].x, half ? v[7].y : v[7].x, b1);
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
-          const uint32_t b0 = int8_to_bf16x2(w[0][d >> 1] >> (d & 1) * 8), b1 = int8_to_bf16x2(w[1][d >> 1] >> (d & 1) * 8);
+          mma_u8s8(c1[4 * half + d], a1, b0[d], b1[d]);
+          mma_u8s8(c2[4 * half + d], a2, b0[d], b1[d]);
+        }
+      }
+      ++since;                                           // (the same in every lane)
+    } else {
+      uint32_t pa[T][2][4];                                // P of 16 keys as an operand
 #pragma unroll
-          for (int i = 0; i < T; ++i) mma_bf16(o[i][4 * half + d], pa[i][b][0], pa[i][b][1], pa[i][b][2], pa[i][b][3], b0, b1);
+      for (int i = 0; i < T; ++i)
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const float ref = m[i][r] == -INFINITY ? 0.0f : m[i][r];
+          const float2 back = make_float2(-ref, -ref);
+          float2 sum = make_float2(0.0f, 0.0f);
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            const float2 d = add2(make_float2(sc[i][r][2 * b], sc[i][r][2 * b + 1]), back), p = make_float2(ex2(d.x), ex2(d.y));
+            sum = add2(sum, p);
+            const float w0 = p.x * vs[2 * b], w1 = p.y * vs[2 * b + 1];
+            pa[i][b >> 1][(b & 1) * 2 + r] = pack_bf16(w0, w1);
+          }
+          l[i][r] += sum.x + sum.y;
+        }
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {                        // 16 keys: 16 b + t, + 4, + 8, + 12
+        uint2 v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int key = 16 * b + t + 4 * e;
+          v[e] = *reinterpret_cast<const uint2*>(s + 2048 + key * 64 + (((g >> 1) ^ (t & 2)) * 16) + (g & 1) * 8);
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {             // four columns: pairs of keys side by side, then one column of both a register
+          uint32_t w[2][2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t x = half ? v[2 * e].y : v[2 * e].x, y = half ? v[2 * e + 1].y : v[2 * e + 1].x;
+            w[e][0] = __byte_perm(x, y, 0x5410);           // columns 0 and 1 of both, then 2 and 3
+            w[e][1] = __byte_perm(x, y, 0x7632);
+          }
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            const uint32_t b0 = int8_to_bf16x2(w[0][d >> 1] >> (d & 1) * 8), b1 = int8_to_bf16x2(w[1][d >> 1] >> (d & 1) * 8);
+#pragma unroll
+            for (int i = 0; i < T; ++i) mma_bf16(o[i][4 * half + d], pa[i][b][0], pa[i][b][1], pa[i][b][2], pa[i][b][3], b0, b1);
+          }
         }
       }
     }
@@ -302,6 +408,7 @@ __global__ void __launch_bounds__(few_warps(ROWS) * 32, 1) k_attn_q8_few(const A
 
   // ---- a warp's result into its stages: O [ROWS][64], the maxima, the sums
   float* mine = reinterpret_cast<float*>(stages);
+  if constexpr (PACK) take_sums(mv == -INFINITY ? 0.0f : ex2(mv - (m[0][0] == -INFINITY ? mv : m[0][0])) * 1.1920928955078125e-07f);   // (2^-23)
 #pragma unroll
   for (int i = 0; i < T; ++i)
 #pragma unroll
@@ -319,7 +426,7 @@ __global__ void __launch_bounds__(few_warps(ROWS) * 32, 1) k_attn_q8_few(const A
           float4 y;
           float* z = &y.x;
 #pragma unroll
-          for (int q = 0; q < 4; ++q) z[q] = PACK ? o[i][d + q][e] + o[i][d + q][e + 2] : o[i][d + q][2 * r + e];
+          for (int q = 0; q < 4; ++q) z[q] = o[i][d + q][2 * r + e];
           *reinterpret_cast<float4*>(mine + row * 64 + 16 * t + 8 * e + d) = y;
         }
     }
@@ -910,7 +1017,14 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
 
 // ---------------------------------------------------------------- host side
 
-constexpr int kManyFrom = 65;          // rows from which the planes are taken
+// Whether a call goes by way of planes, from its time in picoseconds: streaming the cache costs 5 us and 45 ps a cached row, head and 32
+// rows of queries; the planes 11 us, 118 ps a cached row and head, and 25 ps more for each 128 rows of queries after the first.  Fitted to 96 to
+// 512 rows over 512 to 32768 of 16 heads: 96 x 8192 23.6 us against 26.7, 128 x 8192 30.4 against 27.1, 256 x 2048 17.0 against 19.3, 256 x 8192
+// 51.9 against 30.4.
+inline bool attn_q8_by_planes(long long cached, long long rows) {      // cached rows times heads, over all sequences
+  const double x = (double)cached;
+  return 5e6 + 45.0 * x * (double)((rows + 31) / 32) > 11e6 + x * (118.0 + 25.0 * (double)((rows - 1) / kBM));
+}
 
 // How a call is cut: rows a CTA takes (8, 16, 32: the few-row kernel; 128), parts of the cached rows, sequences at once.
 struct AttnQ8Plan {
@@ -922,7 +1036,7 @@ inline AttnQ8Plan attn_q8_plan(int seqs, int M, int H, int HK, int cap) {
   const long long rows = (long long)M * (H / HK);
   A.plane_rows = (cap + kBN - 1) / kBN * kBN;
   const size_t one = (size_t)A.plane_rows * HK * kHD * 4;
-  if (rows >= kManyFrom && one <= kPlanesMost) {
+  if (one <= kPlanesMost && attn_q8_by_planes((long long)seqs * HK * cap, rows)) {
     A.tile = kBM;
     A.seqs = (int)std::max<size_t>(1, std::min<size_t>(seqs, kPlanesAtOnce / one));
     A.planes = one * A.seqs;

@@ -121,6 +121,21 @@ def test_peaked_scores_and_late_maxima(M):
     _check(q, cache)
 
 
+@pytest.mark.parametrize("M", [1, 8, 24, 140])
+def test_weights_that_grow_from_tile_to_tile(M):
+    """Each tile of 32 rows outweighs those before it, by its scores, by its values or by both: the references move in every one."""
+    g = _g(M)
+    rnd = lambda *s: torch.randn(s, generator=g, device="cuda")
+    q = torch.ones((1, M, 64), device="cuda").bfloat16()
+    n = 32 * 40
+    tile = torch.arange(n, device="cuda")[None, :, None] // 32
+    for up_k, up_v in ((12.0, 0), (0.0, 9), (7.0, 2), (20.0, -3)):
+        cache = B.new_cache_q8(1, n, 1)
+        k = rnd(1, n, 64) * 0.1 + up_k / 8 * (tile - 20)
+        B.k_store_q8(cache, k, rnd(1, n, 64) * torch.exp2(up_v * 0.3 * (tile - 20)))
+        _check(q, cache)
+
+
 @pytest.mark.parametrize("M", [1, 20, 150])
 def test_what_lies_in_masked_places(M):
     """NaN blocks and bytes that no store wrote, beyond the length and under the mask, change nothing."""
