@@ -552,12 +552,20 @@ def _here(*tensors: Optional[torch.Tensor]) -> None:
     assert all(t is None or t.get_device() == device for t in tensors), "tensors of another device than the current one"
 
 
+def _new(shape, dtype, device, stream) -> torch.Tensor:
+    """A tensor for a call on `stream` (None: the current one), of that stream's memory: what was given back on another may still be in use there."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def k_norm_q8(x: torch.Tensor, weight=None, bias=None, residual=None, kind=NORM_RMS, eps=1e-6, sum_out=None, q=None, scale=None,
               stream=None):
     """(q int8 like x, scale fp32 [...]): the rows of x [..., C] (+ residual, the sum to sum_out) normalised and quantised."""
     dtype, width = _dtype_of(x), x.shape[-1]
-    q = torch.empty(x.shape, dtype=torch.int8, device=x.device) if q is None else q
-    scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if scale is None else scale
+    q = _new(x.shape, torch.int8, x.device, stream) if q is None else q
+    scale = _new(x.shape[:-1], torch.float32, x.device, stream) if scale is None else scale
     assert all(t.dtype == x.dtype and t.shape == x.shape for t in (residual, sum_out) if t is not None)
     assert all(t.dtype == x.dtype and t.shape == (width,) for t in (weight, bias) if t is not None)
     assert q.dtype == torch.int8 and q.shape == x.shape and scale.dtype == torch.float32 and scale.shape == x.shape[:-1]
@@ -614,7 +622,7 @@ def k_store_q8(cache, k: torch.Tensor, v: torch.Tensor, start=None, stream=None)
 def k_load_q8(cache, n: int, first: int = 0, dtype=torch.bfloat16, stream=None):
     """(k, v) [n_seqs, n, C]: rows first .. first + n - 1 of every sequence, exact."""
     n_seqs, capacity, H = _cache_q8(cache)
-    k, v = (torch.empty((n_seqs, max(n, 0), H * 64), dtype=dtype, device=cache[0].device) for _ in range(2))
+    k, v = (_new((n_seqs, max(n, 0), H * 64), dtype, cache[0].device, stream) for _ in range(2))
     _here(*cache)
     kq, kx, vq, vx = cache
     _check(lib().ovggt_k_load_q8(_dptr(kq), _dptr(kx), _dptr(vq), _dptr(vx), n_seqs, H, capacity, int(first), int(n), _dtype_of(k), _dptr(k),
@@ -629,14 +637,15 @@ def k_attention_q8(q: torch.Tensor, cache, lens=None, live=None, out=None, scrat
     assert q.dtype == torch.bfloat16 and q.dim() == 3 and q.shape[0] == n_seqs and q.shape[2] % 64 == 0
     assert lens is None or (lens.dtype == torch.int32 and lens.shape == (n_seqs,))
     assert live is None or (live.dtype == torch.uint8 and live.shape == (n_seqs, capacity))
-    out = torch.empty_like(q) if out is None else out
+    out = _new(q.shape, q.dtype, q.device, stream) if out is None else out
     assert out.dtype == q.dtype and out.shape == q.shape
     own = status is None
     if own:
-        status = torch.zeros(16, dtype=torch.int32, device=q.device)
+        with torch.cuda.stream(stream):
+            status = torch.zeros(16, dtype=torch.int32, device=q.device)
     need = lib().ovggt_k_attention_q8_scratch_bytes(n_seqs, q.shape[1], q.shape[2] // 64, H, capacity)
     if scratch is None:
-        scratch = torch.empty(need, dtype=torch.uint8, device=q.device)
+        scratch = _new((need,), torch.uint8, q.device, stream)
     assert scratch.numel() * scratch.element_size() >= need
     _here(q, *cache, lens, live, out, scratch, status)
     kq, kx, vq, vx = cache
@@ -644,5 +653,6 @@ def k_attention_q8(q: torch.Tensor, cache, lens=None, live=None, out=None, scrat
                                       _dptr(lens), _dptr(live), _dptr(out), _dptr(scratch), _dptr(status), _stream_ptr(stream)),
            "ovggt_k_attention_q8")
     if own:
-        _check(int(status[0].item()), "ovggt_k_attention_q8 (device status)")
+        with torch.cuda.stream(stream):
+            _check(int(status[0].item()), "ovggt_k_attention_q8 (device status)")
     return out

@@ -828,10 +828,10 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
     bool ok = true;
     // Upper bound of this row's logits in log2 units, |q| |k|_max log2(e) / 8, for the fixed reference (see attn_tcgen05.cuh).
     float bound;
-    bool fixed_ref = false, in_range = false;
+    bool fixed_ref = false, in_range = false, odd;       // odd: a query that is not finite, whose result is NaN anyhow; it does not decide for its warp
     {
       const float kmax2 = __uint_as_float(max(max(max(top[0], top[1]), max(top[2], top[3])), max(max(top[4], top[5]), max(top[6], top[7]))));
-      float qn2 = 0.0f;
+      float qn2 = 0.0f, zero = 0.0f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const uint4 u = *reinterpret_cast<const uint4*>(sQ + row * 128 + ((j ^ (row & 7)) << 4));
@@ -841,9 +841,11 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
           const float lo = __uint_as_float(w[e] << 16), hi = __uint_as_float(w[e] & 0xFFFF0000u);
           qn2 = fmaf(lo, lo, qn2);
           qn2 = fmaf(hi, hi, qn2);
+          zero = fmaf(lo, 0.0f, fmaf(hi, 0.0f, zero));
         }
       }
       bound = sqrtf(qn2 * kmax2) * c;
+      odd = !(zero == 0.0f);
     }
     for (int idx = 0; idx < range[0] && ok; ++idx) {    // idx = 2 * tile + half
       const int it = idx >> 1, hf = idx & 1, left = range[1] - idx * kHalf;
@@ -899,9 +901,9 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
         }
         m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * c;
         // the bound as the reference, a whole number of powers of two above what was seen, where it is not absurdly far above
-        fixed_ref = __all_sync(0xFFFFFFFFu, bound >= m && bound - m <= kFixedRefMaxGap) != 0;
-        if (fixed_ref) m += ceilf(bound - m);
-        in_range = fixed_ref && __all_sync(0xFFFFFFFFu, bound + m <= -1.0f - kPolyLowest) != 0;
+        fixed_ref = __all_sync(0xFFFFFFFFu, odd || (bound >= m && bound - m <= kFixedRefMaxGap)) != 0;
+        if (fixed_ref && !odd) m += ceilf(bound - m);
+        in_range = fixed_ref && __all_sync(0xFFFFFFFFu, odd || bound + m <= -1.0f - kPolyLowest) != 0;
         add = exp_pass(std::false_type{}, std::true_type{}, raw);
       } else if (fixed_ref) {
         add = in_range && left >= kHalf ? exp_pass(std::false_type{}, std::false_type{}, raw) : exp_pass(std::false_type{}, std::true_type{}, raw);

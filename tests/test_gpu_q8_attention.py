@@ -62,14 +62,34 @@ def _check(q, cache, lens=None, live=None):
 SHAPES = [(1, 1, 1, 1, 16), (3, 1, 4, 4, 160), (2, 2, 8, 2, 48), (1, 8, 2, 2, 1008), (4, 3, 12, 4, 336), (2, 5, 8, 2, 112), (1, 17, 3, 3, 320),
           (2, 33, 4, 1, 208), (1, 69, 4, 4, 336), (1, 128, 2, 2, 400), (2, 129, 2, 2, 592), (1, 300, 2, 1, 976), (3, 65, 6, 2, 80), (1, 1, 16, 16, 16400),
           (1, 257, 1, 1, 4112), (5, 1, 8, 1, 2064)]
+# the same by way of bf16 planes: one tile of 128 rows and many, a ragged last one, shared heads, several sequences at once
+PLANES = [(1, 1041, 2, 2, 2720), (3, 700, 2, 1, 1504), (1, 1374, 5, 5, 1376), (20, 300, 8, 2, 400), (2, 333, 3, 1, 4112), (2, 130, 16, 16, 5008)]
 
 
-@pytest.mark.parametrize("seqs,M,heads,kv,capacity", SHAPES)
+def _by_planes(seqs, M, heads, kv, capacity):
+    """Whether a call of these sizes widens the cache into planes (the rule beside the kernels; their bytes are then part of its scratch memory)."""
+    rows, x = M * heads // kv, seqs * kv * capacity
+    rule = 5e6 + 45 * x * -(-rows // 32) > 11e6 + x * (118 + 25 * ((rows - 1) // 128))
+    scratch = B.lib().ovggt_k_attention_q8_scratch_bytes(seqs, M, heads, kv, capacity)
+    assert not rule or scratch >= min(seqs, 8) * capacity * kv * 64 * 4
+    return rule
+
+
+def test_which_sizes_go_by_planes():
+    assert all(_by_planes(*s) for s in PLANES) and not any(_by_planes(*s) for s in SHAPES)
+    assert all(_by_planes(1, M, 1, 1, n) for M, n in ROWS_BY_PLANES)
+
+
+# (tokens, capacity) of a single head and more
+ROWS_BY_PLANES = [(2300, 2608)]
+
+
+@pytest.mark.parametrize("seqs,M,heads,kv,capacity", SHAPES + PLANES)
 def test_whole_caches(seqs, M, heads, kv, capacity):
     _check(*_case(seqs, M, heads, kv, capacity))
 
 
-@pytest.mark.parametrize("seqs,M,heads,kv,capacity", SHAPES)
+@pytest.mark.parametrize("seqs,M,heads,kv,capacity", SHAPES + PLANES)
 def test_lengths_and_masks(seqs, M, heads, kv, capacity):
     q, cache = _case(seqs, M, heads, kv, capacity, seed=7)
     g = _g(capacity)
@@ -80,48 +100,49 @@ def test_lengths_and_masks(seqs, M, heads, kv, capacity):
     _check(q, cache, lens, live)
 
 
-@pytest.mark.parametrize("M", [1, 2, 40, 200])
+@pytest.mark.parametrize("M", [1, 2, 40, 200, 700])
 def test_every_short_length(M):
     """Lengths 0 to 67 and around 192 at once: tiles that end anywhere, and none at all."""
     n = torch.cat([torch.arange(0, 68), torch.arange(189, 197)]).to(torch.int32).cuda()
+    assert _by_planes(len(n), M, 2, 1, 208) == (M >= 200)
     q, cache = _case(len(n), M, 2, 1, 208)
     out = _check(q, cache, n)
     assert not bool(out[0].any())
 
 
-@pytest.mark.parametrize("M", [1, 12, 150])
-def test_lengths_outside_the_cache(M):
-    q, cache = _case(3, M, 2, 2, 48)
-    lens = torch.tensor([-5, 49, 0x7FFFFFFF], dtype=torch.int32, device="cuda")
+@pytest.mark.parametrize("M,capacity", [(1, 48), (12, 48), (150, 48)] + ROWS_BY_PLANES)
+def test_lengths_outside_the_cache(M, capacity):
+    q, cache = _case(3, M, 2, 2, capacity)
+    lens = torch.tensor([-5, capacity + 1, 0x7FFFFFFF], dtype=torch.int32, device="cuda")
     out = B.k_attention_q8(q, cache, lens=lens)
     assert not bool(out[0].any()) and torch.equal(out[1:], B.k_attention_q8(q, cache)[1:])
 
 
-@pytest.mark.parametrize("M", [1, 16, 30, 260])
-def test_one_live_row(M):
+@pytest.mark.parametrize("M,capacity", [(1, 416), (16, 416), (30, 416), (260, 416)] + ROWS_BY_PLANES)
+def test_one_live_row(M, capacity):
     """A single row, wherever it lies, is the result."""
-    q, cache = _case(6, M, 2, 1, 416)
-    live = torch.zeros((6, 416), dtype=torch.uint8, device="cuda")
-    at = [0, 31, 32, 191, 192, 415]
+    q, cache = _case(6, M, 2, 1, capacity)
+    live = torch.zeros((6, capacity), dtype=torch.uint8, device="cuda")
+    at = [0, 31, 32, 191, 192, capacity - 1]
     for s, j in enumerate(at):
         live[s, j] = 255
     out = _check(q, cache, None, live)
-    v = B.k_load_q8(cache, 416)[1]
+    v = B.k_load_q8(cache, capacity)[1]
     for s, j in enumerate(at):
         torch.testing.assert_close(out[s].view(M, 2, 64).double(), v[s, j].double().expand(M, 2, 64), rtol=2.0 ** -7, atol=0)
 
 
-@pytest.mark.parametrize("M", [1, 24, 140])
-def test_peaked_scores_and_late_maxima(M):
+@pytest.mark.parametrize("M,capacity", [(1, 800), (24, 800), (140, 800)] + ROWS_BY_PLANES)
+def test_peaked_scores_and_late_maxima(M, capacity):
     """Scores in the hundreds, their largest in the last rows: every tile moves the reference."""
-    q, cache = _case(2, M, 2, 2, 800, spread=12.0)
-    k, v = B.k_load_q8(cache, 800, dtype=torch.float32)
-    ramp = torch.linspace(0.02, 1, 800, device="cuda")[:, None]
+    q, cache = _case(2, M, 2, 2, capacity, spread=12.0)
+    k, v = B.k_load_q8(cache, capacity, dtype=torch.float32)
+    ramp = torch.linspace(0.02, 1, capacity, device="cuda")[:, None]
     B.k_store_q8(cache, k * ramp, v)
     _check(q, cache)
 
 
-@pytest.mark.parametrize("M", [1, 8, 24, 140])
+@pytest.mark.parametrize("M", [1, 8, 24, 140, 3000])
 def test_weights_that_grow_from_tile_to_tile(M):
     """Each tile of 32 rows outweighs those before it, by its scores, by its values or by both: the references move in every one."""
     g = _g(M)
@@ -136,26 +157,26 @@ def test_weights_that_grow_from_tile_to_tile(M):
         _check(q, cache)
 
 
-@pytest.mark.parametrize("M", [1, 20, 150])
-def test_what_lies_in_masked_places(M):
+@pytest.mark.parametrize("M,capacity", [(1, 224), (20, 224), (150, 224)] + ROWS_BY_PLANES)
+def test_what_lies_in_masked_places(M, capacity):
     """NaN blocks and bytes that no store wrote, beyond the length and under the mask, change nothing."""
-    q, cache = _case(2, M, 4, 2, 224)
-    lens = torch.tensor([150, 224], dtype=torch.int32, device="cuda")
-    live = torch.ones((2, 224), dtype=torch.uint8, device="cuda")
+    q, cache = _case(2, M, 4, 2, capacity)
+    lens = torch.tensor([capacity - 74, capacity], dtype=torch.int32, device="cuda")
+    live = torch.ones((2, capacity), dtype=torch.uint8, device="cuda")
     live[1, 33:90] = 0
     want = B.k_attention_q8(q, cache, lens=lens, live=live)
     for c, fill in zip(cache, (-128, 255, -128, 255)):
         rows = c if c.dtype == torch.int8 else c.transpose(1, 2)
-        rows[0, 150:] = fill
+        rows[0, capacity - 74:] = fill
         rows[1, 33:90] = fill
     assert torch.equal(B.k_attention_q8(q, cache, lens=lens, live=live), want)
 
 
-@pytest.mark.parametrize("M", [1, 9, 21, 150])
+@pytest.mark.parametrize("M,capacity", [(1, 96), (9, 96), (21, 96), (150, 96)] + ROWS_BY_PLANES)
 @pytest.mark.parametrize("side", [1, 3])
-def test_a_live_block_that_is_not_finite(M, side):
+def test_a_live_block_that_is_not_finite(M, capacity, side):
     """... is NaN for the heads that read it, and for them alone."""
-    q, cache = _case(2, M, 4, 2, 96)
+    q, cache = _case(2, M, 4, 2, capacity)
     want = B.k_attention_q8(q, cache)
     cache[side - 1][1, 40, 64:] = 0
     cache[side][1, 1, 40] = 255
@@ -165,9 +186,9 @@ def test_a_live_block_that_is_not_finite(M, side):
     assert torch.equal(out[0], want[0]) and torch.equal(out[1, :, :2], want[1, :, :2])
 
 
-@pytest.mark.parametrize("M", [3, 9, 21, 150])
-def test_queries_that_are_not_finite(M):
-    q, cache = _case(1, M, 2, 2, 96)
+@pytest.mark.parametrize("M,capacity", [(3, 96), (9, 96), (21, 96), (150, 96)] + ROWS_BY_PLANES)
+def test_queries_that_are_not_finite(M, capacity):
+    q, cache = _case(1, M, 2, 2, capacity)
     want = B.k_attention_q8(q, cache)
     q[0, 1, 3], q[0, 2, 64] = float("nan"), float("inf")
     out = B.k_attention_q8(q, cache)
@@ -177,14 +198,14 @@ def test_queries_that_are_not_finite(M):
     assert not bool(B.k_attention_q8(q, cache, lens=torch.zeros(1, dtype=torch.int32, device="cuda")).any())
 
 
-@pytest.mark.parametrize("M", [1, 20, 150])
-def test_small_and_large_exponents(M):
+@pytest.mark.parametrize("M,capacity", [(1, 64), (20, 64), (150, 64)] + ROWS_BY_PLANES)
+def test_small_and_large_exponents(M, capacity):
     """Keys and values far from one: the powers of two meet without leaving fp32's range on the way."""
     g = _g(M)
     q = torch.randn((1, M, 64), generator=g, device="cuda")
     for up in (100, -100):
-        cache = B.new_cache_q8(1, 64, 1)
-        k, v = torch.randn((1, 64, 64), generator=g, device="cuda"), torch.randn((1, 64, 64), generator=g, device="cuda")
+        cache = B.new_cache_q8(1, capacity, 1)
+        k, v = torch.randn((1, capacity, 64), generator=g, device="cuda"), torch.randn((1, capacity, 64), generator=g, device="cuda")
         B.k_store_q8(cache, k * 2.0 ** up, v * 2.0 ** up)
         _check((q * 2.0 ** -up).bfloat16(), cache)
 
@@ -209,9 +230,9 @@ def test_offsets_past_32_bits(M, live_rows):
     assert bool(((out.double() - ref).abs() <= tol).all())
 
 
-@pytest.mark.parametrize("M", [1, 12, 150])
-def test_same_bits_again_and_beside_another_call(M):
-    q, cache = _case(3, M, 4, 2, 608)
+@pytest.mark.parametrize("M,capacity", [(1, 608), (12, 608), (150, 608)] + ROWS_BY_PLANES)
+def test_same_bits_again_and_beside_another_call(M, capacity):
+    q, cache = _case(3, M, 4, 2, capacity)
     want = B.k_attention_q8(q, cache)
     other = torch.cuda.Stream()
     other.wait_stream(torch.cuda.current_stream())
