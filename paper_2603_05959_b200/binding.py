@@ -540,16 +540,22 @@ def k_attention(q, k, v, n_heads: int, out=None, scratch=None, status=None, stre
 
 
 # ------------------------------------------------------------------ a block in 8 bits
+# (The smallest of these calls take the GPU less time than Python: arguments are checked without generators, each tensor once.)
+
+_I8, _U8, _I32, _F32, _BF16 = torch.int8, torch.uint8, torch.int32, torch.float32, torch.bfloat16
+
 
 def _dtype_of(t: torch.Tensor) -> int:
-    assert t.dtype in (torch.float32, torch.bfloat16)
-    return DTYPE_F32 if t.dtype == torch.float32 else DTYPE_BF16
+    assert t.dtype is _F32 or t.dtype is _BF16
+    return DTYPE_F32 if t.dtype is _F32 else DTYPE_BF16
 
 
-def _here(*tensors: Optional[torch.Tensor]) -> None:
-    """The kernels run on the current device: so do their tensors."""
-    device = torch._C._cuda_getDevice()
-    assert all(t is None or t.get_device() == device for t in tensors), "tensors of another device than the current one"
+def _at(t: Optional[torch.Tensor], device: int) -> Optional[int]:
+    """The address of a contiguous tensor of the current device, which the kernels run on (None: none)."""
+    if t is None:
+        return None
+    assert t.get_device() == device and t.is_contiguous()
+    return t.data_ptr()
 
 
 def _new(shape, dtype, device, stream) -> torch.Tensor:
@@ -563,31 +569,43 @@ def _new(shape, dtype, device, stream) -> torch.Tensor:
 def k_norm_q8(x: torch.Tensor, weight=None, bias=None, residual=None, kind=NORM_RMS, eps=1e-6, sum_out=None, q=None, scale=None,
               stream=None):
     """(q int8 like x, scale fp32 [...]): the rows of x [..., C] (+ residual, the sum to sum_out) normalised and quantised."""
-    dtype, width = _dtype_of(x), x.shape[-1]
-    q = _new(x.shape, torch.int8, x.device, stream) if q is None else q
-    scale = _new(x.shape[:-1], torch.float32, x.device, stream) if scale is None else scale
-    assert all(t.dtype == x.dtype and t.shape == x.shape for t in (residual, sum_out) if t is not None)
-    assert all(t.dtype == x.dtype and t.shape == (width,) for t in (weight, bias) if t is not None)
-    assert q.dtype == torch.int8 and q.shape == x.shape and scale.dtype == torch.float32 and scale.shape == x.shape[:-1]
-    _here(x, weight, bias, residual, sum_out, q, scale)
-    _check(lib().ovggt_k_norm_q8(_dptr(x), _dptr(residual), _dptr(weight), _dptr(bias), x.numel() // width if width else 0, width, dtype, kind, eps,
-                                 _dptr(sum_out), _dptr(q), _dptr(scale), _stream_ptr(stream)), "ovggt_k_norm_q8")
+    t, shape = x.dtype, x.shape
+    dtype, width = _dtype_of(x), shape[-1]
+    if q is None:
+        q = _new(shape, _I8, x.device, stream)
+    if scale is None:
+        scale = _new(shape[:-1], _F32, x.device, stream)
+    assert residual is None or (residual.dtype is t and residual.shape == shape)
+    assert sum_out is None or (sum_out.dtype is t and sum_out.shape == shape)
+    assert weight is None or (weight.dtype is t and weight.shape == (width,))
+    assert bias is None or (bias.dtype is t and bias.shape == (width,))
+    assert q.dtype is _I8 and q.shape == shape and scale.dtype is _F32 and scale.shape == shape[:-1]
+    d = torch._C._cuda_getDevice()
+    code = lib().ovggt_k_norm_q8(_at(x, d), _at(residual, d), _at(weight, d), _at(bias, d), x.numel() // width if width else 0, width, dtype, kind,
+                                 eps, _at(sum_out, d), _at(q, d), _at(scale, d), _stream_ptr(stream))
+    if code:
+        _check(code, "ovggt_k_norm_q8")
     return q, scale
 
 
 def k_linear_q8(a, a_scale, w, w_scale, outs=(), gelu=False, residual=None, sum_out=None, status=None, stream=None) -> None:
     """t = (a a_scale) [M, K] @ (w w_scale) [N, K] ^T (then GELU), int8 operands; its column blocks to outs; sum_out = residual + t.
     Nothing is allocated."""
-    (M, K), N = a.shape, w.shape[0]
-    assert w.shape[1] == K and a.dtype == torch.int8 and w.dtype == torch.int8
-    assert a_scale.shape == (M,) and w_scale.shape == (N,) and a_scale.dtype == torch.float32 and w_scale.dtype == torch.float32
-    assert all(t.dtype == torch.bfloat16 for t in (residual, sum_out, *outs) if t is not None)
-    assert all(o.numel() * len(outs) == M * N for o in outs) and len(outs) <= 3
-    assert all(t.numel() == M * N for t in (residual, sum_out) if t is not None) and status.numel() * status.element_size() >= 4
-    _here(a, a_scale, w, w_scale, residual, sum_out, status, *outs)
-    _check(lib().ovggt_k_linear_q8(_dptr(a), _dptr(a_scale), _dptr(w), _dptr(w_scale), M, N, K, (C.c_void_p * 3)(*[_dptr(o) for o in outs]),
-                                   len(outs), int(gelu), _dptr(residual), _dptr(sum_out), _dptr(status), _stream_ptr(stream)),
-           "ovggt_k_linear_q8")
+    (M, K), N, n = a.shape, w.shape[0], len(outs)
+    assert w.shape[1] == K and a.dtype is _I8 and w.dtype is _I8
+    assert a_scale.shape == (M,) and w_scale.shape == (N,) and a_scale.dtype is _F32 and w_scale.dtype is _F32
+    assert n <= 3 and status.numel() * status.element_size() >= 4
+    d = torch._C._cuda_getDevice()
+    at = (C.c_void_p * 3)()
+    for i, o in enumerate(outs):
+        assert o.dtype is _BF16 and o.numel() * n == M * N
+        at[i] = _at(o, d)
+    for t in (residual, sum_out):
+        assert t is None or (t.dtype is _BF16 and t.numel() == M * N)
+    code = lib().ovggt_k_linear_q8(_at(a, d), _at(a_scale, d), _at(w, d), _at(w_scale, d), M, N, K, at, n, int(gelu), _at(residual, d),
+                                   _at(sum_out, d), _at(status, d), _stream_ptr(stream))
+    if code:
+        _check(code, "ovggt_k_linear_q8")
 
 
 def new_cache_q8(n_seqs: int, capacity: int, n_heads: int, device=None):
@@ -595,14 +613,14 @@ def new_cache_q8(n_seqs: int, capacity: int, n_heads: int, device=None):
     device = device or torch.device("cuda", torch.cuda.current_device())
     rows = (capacity + 15) // 16 * 16
     new = lambda *shape, dtype: torch.zeros(shape, dtype=dtype, device=device)
-    return (new(n_seqs, rows, n_heads * 64, dtype=torch.int8), new(n_seqs, n_heads, rows, dtype=torch.uint8),
-            new(n_seqs, rows, n_heads * 64, dtype=torch.int8), new(n_seqs, n_heads, rows, dtype=torch.uint8))
+    return (new(n_seqs, rows, n_heads * 64, dtype=_I8), new(n_seqs, n_heads, rows, dtype=_U8),
+            new(n_seqs, rows, n_heads * 64, dtype=_I8), new(n_seqs, n_heads, rows, dtype=_U8))
 
 
 def _cache_q8(cache):
     """(n_seqs, capacity, n_heads) of an 8-bit cache's four tensors."""
     kq, kx, vq, vx = cache
-    assert kq.dtype == vq.dtype == torch.int8 and kx.dtype == vx.dtype == torch.uint8
+    assert kq.dtype is _I8 and vq.dtype is _I8 and kx.dtype is _U8 and vx.dtype is _U8
     n_seqs, capacity, width = kq.shape
     assert width % 64 == 0 and vq.shape == kq.shape and kx.shape == vx.shape == (n_seqs, width // 64, capacity)
     return n_seqs, capacity, width // 64
@@ -611,22 +629,27 @@ def _cache_q8(cache):
 def k_store_q8(cache, k: torch.Tensor, v: torch.Tensor, start=None, stream=None) -> None:
     """Rows k, v [n_seqs, M, C] into the cache (kq, kx, vq, vx), from row start[s] (int32 [n_seqs]; None: 0) of each sequence on."""
     n_seqs, capacity, H = _cache_q8(cache)
-    assert k.shape == v.shape and k.dtype == v.dtype and k.dim() == 3 and (k.shape[0], k.shape[2]) == (n_seqs, H * 64)
-    assert start is None or (start.dtype == torch.int32 and start.shape == (n_seqs,))
-    _here(*cache, k, v, start)
     kq, kx, vq, vx = cache
-    _check(lib().ovggt_k_store_q8(_dptr(k), _dptr(v), n_seqs, k.shape[1], H, _dtype_of(k), _dptr(start), capacity, _dptr(kq), _dptr(kx),
-                                  _dptr(vq), _dptr(vx), _stream_ptr(stream)), "ovggt_k_store_q8")
+    assert k.dim() == 3 and k.shape[0] == n_seqs and k.shape[2] == H * 64 and k.shape == v.shape and k.dtype is v.dtype
+    assert start is None or (start.dtype is _I32 and start.shape == (n_seqs,))
+    d = torch._C._cuda_getDevice()
+    code = lib().ovggt_k_store_q8(_at(k, d), _at(v, d), n_seqs, k.shape[1], H, _dtype_of(k), _at(start, d), capacity, _at(kq, d), _at(kx, d),
+                                  _at(vq, d), _at(vx, d), _stream_ptr(stream))
+    if code:
+        _check(code, "ovggt_k_store_q8")
 
 
 def k_load_q8(cache, n: int, first: int = 0, dtype=torch.bfloat16, stream=None):
     """(k, v) [n_seqs, n, C]: rows first .. first + n - 1 of every sequence, exact."""
     n_seqs, capacity, H = _cache_q8(cache)
-    k, v = (_new((n_seqs, max(n, 0), H * 64), dtype, cache[0].device, stream) for _ in range(2))
-    _here(*cache)
     kq, kx, vq, vx = cache
-    _check(lib().ovggt_k_load_q8(_dptr(kq), _dptr(kx), _dptr(vq), _dptr(vx), n_seqs, H, capacity, int(first), int(n), _dtype_of(k), _dptr(k),
-                                 _dptr(v), _stream_ptr(stream)), "ovggt_k_load_q8")
+    shape = (n_seqs, max(n, 0), H * 64)
+    k, v = _new(shape, dtype, kq.device, stream), _new(shape, dtype, kq.device, stream)
+    d = torch._C._cuda_getDevice()
+    code = lib().ovggt_k_load_q8(_at(kq, d), _at(kx, d), _at(vq, d), _at(vx, d), n_seqs, H, capacity, int(first), int(n), _dtype_of(k), _at(k, d),
+                                 _at(v, d), _stream_ptr(stream))
+    if code:
+        _check(code, "ovggt_k_load_q8")
     return k, v
 
 
@@ -634,24 +657,29 @@ def k_attention_q8(q: torch.Tensor, cache, lens=None, live=None, out=None, scrat
     """softmax(q k / 8) v of queries q [n_seqs, M, heads * 64] (bf16) over the cache's live rows (uint8 [n_seqs, capacity]; None: all)
     within lens (int32 [n_seqs]; None: the capacity); 0 where there is none."""
     n_seqs, capacity, H = _cache_q8(cache)
-    assert q.dtype == torch.bfloat16 and q.dim() == 3 and q.shape[0] == n_seqs and q.shape[2] % 64 == 0
-    assert lens is None or (lens.dtype == torch.int32 and lens.shape == (n_seqs,))
-    assert live is None or (live.dtype == torch.uint8 and live.shape == (n_seqs, capacity))
-    out = _new(q.shape, q.dtype, q.device, stream) if out is None else out
-    assert out.dtype == q.dtype and out.shape == q.shape
+    kq, kx, vq, vx = cache
+    shape = q.shape
+    assert q.dtype is _BF16 and len(shape) == 3 and shape[0] == n_seqs and shape[2] % 64 == 0
+    assert lens is None or (lens.dtype is _I32 and lens.shape == (n_seqs,))
+    assert live is None or (live.dtype is _U8 and live.shape == (n_seqs, capacity))
+    M, heads = shape[1], shape[2] // 64
+    if out is None:
+        out = _new(shape, _BF16, q.device, stream)
+    assert out.dtype is _BF16 and out.shape == shape
     own = status is None
     if own:
         with torch.cuda.stream(stream):
-            status = torch.zeros(16, dtype=torch.int32, device=q.device)
-    need = lib().ovggt_k_attention_q8_scratch_bytes(n_seqs, q.shape[1], q.shape[2] // 64, H, capacity)
+            status = torch.zeros(16, dtype=_I32, device=q.device)
+    L = lib()
+    need = L.ovggt_k_attention_q8_scratch_bytes(n_seqs, M, heads, H, capacity)
     if scratch is None:
-        scratch = _new((need,), torch.uint8, q.device, stream)
-    assert scratch.numel() * scratch.element_size() >= need
-    _here(q, *cache, lens, live, out, scratch, status)
-    kq, kx, vq, vx = cache
-    _check(lib().ovggt_k_attention_q8(_dptr(q), _dptr(kq), _dptr(kx), _dptr(vq), _dptr(vx), n_seqs, q.shape[1], q.shape[2] // 64, H, capacity,
-                                      _dptr(lens), _dptr(live), _dptr(out), _dptr(scratch), _dptr(status), _stream_ptr(stream)),
-           "ovggt_k_attention_q8")
+        scratch = _new((need,), _U8, q.device, stream)
+    assert scratch.numel() * scratch.element_size() >= need and status.numel() * status.element_size() >= 4
+    d = torch._C._cuda_getDevice()
+    code = L.ovggt_k_attention_q8(_at(q, d), _at(kq, d), _at(kx, d), _at(vq, d), _at(vx, d), n_seqs, M, heads, H, capacity, _at(lens, d),
+                                  _at(live, d), _at(out, d), _at(scratch, d), _at(status, d), _stream_ptr(stream))
+    if code:
+        _check(code, "ovggt_k_attention_q8")
     if own:
         with torch.cuda.stream(stream):
             _check(int(status[0].item()), "ovggt_k_attention_q8 (device status)")
