@@ -382,7 +382,7 @@ int ovggt_k_norm_q8(const void* x, const void* residual, const void* weight, con
 
 /* The product of ovggt_k_linear_bf16 on int8 rows: t = bf16(a_scale[m] w_scale[n] sum_k A[m, k] W[n, k]), A [M, K], W [N, K] (a row of
  * weights for each channel), a_scale [M], w_scale [N] fp32; the sums are int32 and exact.  gelu, outs, n_outs, residual, sum and
- * device_status as there (sum may be residual here).  K a multiple of 16, up to 131056; N a multiple of 8 (OVGGT_ERR_UNSUPPORTED). */
+ * device_status as there (sum may be residual here), but for GELU's relative error before its rounding, 1e-5 (and 1e-18 below -9).  K a multiple of 16, up to 131056; N a multiple of 8 (OVGGT_ERR_UNSUPPORTED). */
 int ovggt_k_linear_q8(const int8_t* A, const float* a_scale, const int8_t* W, const float* w_scale, int32_t M, int32_t N, int32_t K,
                       void* const* outs, int32_t n_outs, int32_t gelu, const void* residual, void* sum, int32_t* device_status,
                       void* stream);

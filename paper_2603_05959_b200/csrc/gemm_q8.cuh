@@ -28,6 +28,36 @@ __device__ __forceinline__ void mma_s8_first(int (&c)[4], uint32_t a0, uint32_t 
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "r"(0));
 }
 
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n .reg .b64 ra, rb, rd;\n mov.b64 ra, {%2, %3};\n mov.b64 rb, {%4, %5};\n mul.rn.f32x2 rd, ra, rb;\n mov.b64 {%0, %1}, rd;\n}\n"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+// max(x, 0), NaN for NaN
+__device__ __forceinline__ float positive(float x) {
+  float y;
+  asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(y) : "f"(x));
+  return y;
+}
+// x Phi(x) of a pair of bf16 values, rounded to bf16: max(x, 0) - n Phi(-n) with n = |x|, at most 9 (where n Phi(-n) is 1e-18), and log2 Phi(t) as a
+// polynomial of degree 8 on [-9, 0] in u = 1 + 2 t / 9 (through a weighted fit at Chebyshev nodes; relative error of the result before its
+// rounding, over all bf16 values above -9, 8.7e-6).  One way for all values, 21 instructions a pair: by error functions below -3, as the bf16
+// product does for the sake of its bits, 10992 x 4096 x 1024 with values of deviation 3 takes 82 us instead of 58.
+__device__ __forceinline__ uint32_t gelu_near(uint32_t w) {
+  const float2 x = make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+  const float2 t = make_float2(fmaxf(-fabsf(x.x), -9.0f), fmaxf(-fabsf(x.y), -9.0f));
+  const float2 u = fma2(t, make_float2(0.2222222222f, 0.2222222222f), make_float2(1.0f, 1.0f));
+  constexpr float k[9] = {-18.167024612426758f, 30.540971755981445f, -14.040131568908691f, 0.30345144867897034f, 0.16877345740795135f,
+                          0.09042360633611679f, 0.054782647639513016f, 0.036208659410476685f, 0.01254955492913723f};
+  float2 q = make_float2(k[8], k[8]);
+#pragma unroll
+  for (int i = 7; i >= 0; --i) q = fma2(q, u, make_float2(k[i], k[i]));
+  const float2 r = fma2(t, make_float2(ex2(q.x), ex2(q.y)), make_float2(positive(x.x), positive(x.y)));
+  return pack_bf16(r.x, r.y);
+}
+
 // Eight sums of row m, columns [n, n + 8), finished and stored.
 __device__ __forceinline__ void q8_finish8(const GemmQ8Args& P, int m, int n, const int* acc) {
   const float as = P.a_scale[m];
@@ -38,7 +68,7 @@ __device__ __forceinline__ void q8_finish8(const GemmQ8Args& P, int m, int n, co
   for (int e = 0; e < 4; ++e) w[e] = pack_bf16((float)acc[2 * e] * as * s[2 * e], (float)acc[2 * e + 1] * as * s[2 * e + 1]);
   if (P.o.gelu) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = pack_bf16(gelu(__uint_as_float(w[e] << 16)), gelu(__uint_as_float(w[e] & 0xFFFF0000u)));
+    for (int e = 0; e < 4; ++e) w[e] = gelu_near(w[e]);
   }
   const uint4 t = make_uint4(w[0], w[1], w[2], w[3]);
   if (P.o.residual != nullptr)
@@ -273,10 +303,15 @@ k_linear_q8_tcgen05(const __grid_constant__ CUtensorMap tm_a, const __grid_const
           for (int e = 0; e < 4; ++e) {                                        // (N a multiple of 8: scales past it are not read)
             const int n = col + h + 4 * e;
             const float4 ws = n < P.o.N ? __ldg(reinterpret_cast<const float4*>(P.w_scale + n)) : make_float4(0.f, 0.f, 0.f, 0.f);
-            w[2 * e] = pack_bf16((float)(int)o[4 * e] * as * ws.x, (float)(int)o[4 * e + 1] * as * ws.y);
-            w[2 * e + 1] = pack_bf16((float)(int)o[4 * e + 2] * as * ws.z, (float)(int)o[4 * e + 3] * as * ws.w);
+            const float2 x = mul2(mul2(make_float2((float)(int)o[4 * e], (float)(int)o[4 * e + 1]), make_float2(as, as)), make_float2(ws.x, ws.y));
+            const float2 y = mul2(mul2(make_float2((float)(int)o[4 * e + 2], (float)(int)o[4 * e + 3]), make_float2(as, as)), make_float2(ws.z, ws.w));
+            w[2 * e] = pack_bf16(x.x, x.y);
+            w[2 * e + 1] = pack_bf16(y.x, y.y);
           }
-          if constexpr (GELU) gelu_warp(w);
+          if constexpr (GELU) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = gelu_near(w[e]);
+          }
 #pragma unroll
           for (int u = 0; u < 2; ++u)
             stage[lane * kUnits + ((h / 8 + u) ^ (lane & (kUnits - 1)))] = make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
@@ -321,15 +356,26 @@ static inline int q8_tcgen05_launch(const GemmQ8Args& P, cudaStream_t st) {
   return OVGGT_OK;
 }
 
-constexpr int kQ8Few = 32;             // tokens up to which the few-token kernel is taken
+constexpr int kQ8Few = 32;             // tokens up to which the few-token kernel is taken (32 x 4096 x 1024: 4.9 us, by tiles 5.1; 64: 9 and 4.7)
+
+// Tile width, from a model in nanoseconds fitted to 718 to 10992 tokens, 768 to 4096 channels and columns: set-up and last epilogue, waves
+// over 148 SMs as long as their steps of 128 columns, and what is left of an epilogue between two tiles.  1374 x 4096 x 1024 takes 15.2, 12.9
+// and 14.8 us with tiles of 256, 128 and 64 channels, 1374 x 1024 x 4096 16.6, 12.5 and 17.6, 10992 x 4096 x 1024 58, 60 and 87.
+inline int q8_tile_width(int M, int N, int K) {
+  const long tiles_m = (M + 127) / 128, steps = (K + kQ8K - 1) / kQ8K;
+  auto ns = [&](int bn, long step, long set_up, long between) {
+    const long waves = (tiles_m * ((N + bn - 1) / bn) + 147) / 148;
+    return set_up + waves * steps * step + (waves - 1) * between;
+  };
+  const long wide = ns(256, 400, 7600, 1200), middle = ns(128, 270, 5000, 700), narrow = ns(64, 250, 4000, 200);
+  return wide <= middle && wide <= narrow ? 256 : (middle <= narrow ? 128 : 64);
+}
 
 static inline int gemm_q8_launch(const GemmQ8Args& P, cudaStream_t st) {
   const int M = P.o.M;
   if (M > kQ8Few) {
-    const long tiles_m = (M + 127) / 128;
-    if (tiles_m * ((P.o.N + 255) / 256) >= 148) return q8_tcgen05_launch<256>(P, st);
-    if (tiles_m * ((P.o.N + 127) / 128) >= 100) return q8_tcgen05_launch<128>(P, st);
-    return q8_tcgen05_launch<64>(P, st);
+    const int bn = q8_tile_width(M, P.o.N, P.o.K);
+    return bn == 256 ? q8_tcgen05_launch<256>(P, st) : (bn == 128 ? q8_tcgen05_launch<128>(P, st) : q8_tcgen05_launch<64>(P, st));
   }
   const int groups = M <= 8 ? 1 : (M <= 16 ? 2 : 4);
   const auto kernel = groups == 1 ? k_linear_q8_few<1> : (groups == 2 ? k_linear_q8_few<2> : k_linear_q8_few<4>);

@@ -27,6 +27,13 @@ def _t(a, as_, w, ws):
     return ((a.double() @ w.double().T).float() * as_[:, None] * ws).bfloat16()
 
 
+def _check_gelu(t, x):
+    """t against GELU of bf16 x in fp64: 1e-5 of the value from the polynomial and its fp32 evaluation, the result's own rounding (2^-8, down to
+    bf16's smallest step), and 1e-17 where it is cut off, below -9."""
+    ref = 0.5 * x.double() * torch.special.erfc(-x.double() / 2 ** 0.5)        # (not by ndtr, which cancels in the tail)
+    assert bool(((t.double() - ref).abs() <= (2.0 ** -8 + 1e-5) * ref.abs() + 2.0 ** -134 + 1e-17 * (x < -9)).all())
+
+
 @pytest.mark.parametrize("M,N,K", SHAPES)
 def test_linear(M, N, K):
     a, as_, w, ws, x, st = _case(M, N, K)
@@ -41,13 +48,35 @@ def test_linear(M, N, K):
     B.k_linear_q8(a, as_, w, ws, (), residual=x, sum_out=x, status=st)
     assert torch.equal(s, x)                             # (the residual stream in place)
     B.k_linear_q8(a, as_, w, ws, (t,), gelu=True, status=st)
-    assert torch.equal(t, torch.nn.functional.gelu(ref))
+    _check_gelu(t, ref)
     for n in (2, 3):
         if N % (8 * n) == 0:
             parts = [torch.empty((M, N // n), dtype=torch.bfloat16, device="cuda") for _ in range(n)]
             B.k_linear_q8(a, as_, w, ws, parts, status=st)
             assert torch.equal(torch.cat(parts, 1), ref)
     assert int(st[0]) == 0
+
+
+@pytest.mark.parametrize("tiles", [False, True])
+def test_gelu_over_its_range(tiles):
+    """Every bf16 value there is, as the scale of a product with one: few tokens and many."""
+    v = torch.arange(-2 ** 15, 2 ** 15, device="cuda").to(torch.int16).view(torch.bfloat16)
+    v = v[:, None] if not tiles else torch.cat([v, v[:40]])[:, None]
+    for lo in range(0, len(v), 2 ** 14):
+        x = v[lo:lo + 2 ** 14].contiguous() if tiles else v[lo:lo + 2 ** 14]
+        scale = x.float().view(-1)
+        one = torch.zeros((8, 16), dtype=torch.int8, device="cuda")
+        one[:, 0] = 1
+        st = torch.zeros(16, dtype=torch.int32, device="cuda")
+        step = len(scale) if tiles else 32
+        out = torch.empty((len(scale), 8), dtype=torch.bfloat16, device="cuda")
+        for i in range(0, len(scale), step):
+            n = min(step, len(scale) - i)
+            B.k_linear_q8(one[:1].expand(n, 16).contiguous(), scale[i:i + n].contiguous(), one, torch.ones(8, device="cuda"), (out[i:i + n],), gelu=True, status=st)
+        x = x.view(-1, 1).expand(-1, 8)
+        fine = x.isfinite()
+        _check_gelu(out[fine], x[fine])
+        assert bool(out[x.isnan()].isnan().all()) and bool((out[x == float("inf")] == float("inf")).all()) and bool((out[x == -float("inf")].abs() <= 1e-17).all())
 
 
 @pytest.mark.parametrize("M", [1, 40, 700])
