@@ -36,11 +36,11 @@ __device__ __forceinline__ void load8(const uint4* p, size_t unit, float* f) {  
   }
 }
 
-// A value over the THREADS threads that hold a row: a warp's butterfly, then the warps' results in order.
+// A value over the THREADS threads that hold a row: a butterfly, then the warps' results in order.
 template <int THREADS, typename Op>
 __device__ __forceinline__ float row_reduce(float x, float* sh, Op op) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x = op(x, __shfl_xor_sync(0xFFFFFFFFu, x, o));
+  for (int o = (THREADS < 32 ? THREADS : 32) / 2; o > 0; o >>= 1) x = op(x, __shfl_xor_sync(0xFFFFFFFFu, x, o));
   if constexpr (THREADS > 32) {
     __syncthreads();                                     // (the scratch of the reduction before has been read)
     if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = x;
@@ -52,48 +52,61 @@ __device__ __forceinline__ float row_reduce(float x, float* sh, Op op) {
   return x;
 }
 
-// UNITS groups of eight elements a thread, THREADS threads a row: a warp, or a CTA of 128 or 256.
-constexpr int kNormWarps = 4;                            // rows of a CTA where a warp takes a row
-template <int DT, int THREADS, int UNITS>
-__global__ void __launch_bounds__(THREADS == 32 ? kNormWarps * 32 : THREADS) k_norm_q8(const NormQ8Args P) {
-  __shared__ float sh[8];
+// Four groups of eight elements a thread, whatever the row's width: 8 to 512 threads a row, several rows a CTA where they are less than
+// 128.  All loads, the weight's among them, are requested before the first reduction.  What bounds it is memory (10992 x 1024 bf16 with a
+// residual: 79 MB), of a single row the trip to it: with one to four groups a thread, a warp up to 1024 columns and a CTA beyond, and weights
+// read where they are needed, 60000 x 256 took 23.6 us, 10992 x 4096 30.7 and one row of 1024 3.5.
+constexpr int kNormUnits = 4;
+__host__ __device__ constexpr int norm_cta(int threads) { return threads < 128 ? (threads == 64 ? 64 : 128) : threads; }
+template <int DT, int THREADS>
+__global__ void __launch_bounds__(norm_cta(THREADS)) k_norm_q8(const NormQ8Args P) {
+  __shared__ float sh[16];
+  constexpr int U = kNormUnits, kWords = DT == kBF16 ? 1 : 2;                 // 16-byte words of a group
   pdl_trigger();
   pdl_wait();
-  const int tid = THREADS == 32 ? threadIdx.x & 31 : threadIdx.x;
-  const long long row = THREADS == 32 ? (long long)blockIdx.x * kNormWarps + (threadIdx.x >> 5) : blockIdx.x;
-  if (THREADS == 32 && row >= P.rows) return;
+  const int tid = threadIdx.x % THREADS;
+  const long long row = (long long)blockIdx.x * (norm_cta(THREADS) / THREADS) + threadIdx.x / THREADS;
+  const bool in = THREADS > 32 || row < P.rows;          // (a warp's rows go through its shuffles together)
   const int units = P.C / 8;
   const size_t u0 = (size_t)row * units;
-  float y[UNITS][8];
+  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+  uint4 x[U][kWords], r[U][kWords], w[U][kWords];
 #pragma unroll
-  for (int i = 0; i < UNITS; ++i) {
-    const int u = tid + i * THREADS;
+  for (int i = 0; i < U; ++i)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[i][e] = 0.0f;
-    if (u < units) load8<DT>(P.x, u0 + u, y[i]);
-  }
-  if (P.residual != nullptr) {
-#pragma unroll
-    for (int i = 0; i < UNITS; ++i) {
+    for (int j = 0; j < kWords; ++j) {
       const int u = tid + i * THREADS;
-      if (u < units) {
-        float r[8];
-        load8<DT>(P.residual, u0 + u, r);
-        if constexpr (DT == kBF16) {
-          uint4 s;
-          uint32_t* w = reinterpret_cast<uint32_t*>(&s);
+      const bool here = in && u < units;
+      x[i][j] = here ? P.x[(u0 + u) * kWords + j] : zero;
+      r[i][j] = here && P.residual != nullptr ? P.residual[(u0 + u) * kWords + j] : zero;
+      w[i][j] = u < units && P.weight != nullptr ? P.weight[(size_t)u * kWords + j] : zero;
+    }
+  auto eight = [](const uint4 (&v)[kWords], float* f) {
+    unpack<DT>(v[0], f);
+    if constexpr (DT != kBF16) unpack<DT>(v[kWords - 1], f + 4);
+  };
+  float y[U][8];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] = pack_bf16(y[i][2 * e] + r[2 * e], y[i][2 * e + 1] + r[2 * e + 1]);
-          unpack<DT>(s, y[i]);                           // (the norm is that of the stored sum)
-          if (P.sum != nullptr) P.sum[u0 + u] = s;
-        } else {
+  for (int i = 0; i < U; ++i) {
+    eight(x[i], y[i]);
+    if (P.residual != nullptr) {
+      float b[8];
+      eight(r[i], b);
+      uint4 s[kWords];
+      if constexpr (DT == kBF16) {
+        uint32_t* o = reinterpret_cast<uint32_t*>(s);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) y[i][e] += r[e];
-          if (P.sum != nullptr) {
-            reinterpret_cast<float4*>(P.sum)[2 * (u0 + u)] = make_float4(y[i][0], y[i][1], y[i][2], y[i][3]);
-            reinterpret_cast<float4*>(P.sum)[2 * (u0 + u) + 1] = make_float4(y[i][4], y[i][5], y[i][6], y[i][7]);
-          }
-        }
+        for (int e = 0; e < 4; ++e) o[e] = pack_bf16(y[i][2 * e] + b[2 * e], y[i][2 * e + 1] + b[2 * e + 1]);
+      } else {
+        float* o = reinterpret_cast<float*>(s);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = y[i][e] + b[e];
+      }
+      eight(s, y[i]);                                    // (the norm is that of the stored sum)
+      const int u = tid + i * THREADS;
+      if (P.sum != nullptr && in && u < units) {
+#pragma unroll
+        for (int j = 0; j < kWords; ++j) P.sum[(u0 + u) * kWords + j] = s[j];
       }
     }
   }
@@ -102,12 +115,12 @@ __global__ void __launch_bounds__(THREADS == 32 ? kNormWarps * 32 : THREADS) k_n
     if (P.kind == OVGGT_NORM_LAYER) {
       float s = 0.0f;
 #pragma unroll
-      for (int i = 0; i < UNITS; ++i)
+      for (int i = 0; i < U; ++i)
 #pragma unroll
         for (int e = 0; e < 8; ++e) s += y[i][e];
       const float mean = row_reduce<THREADS>(s, sh, add) / (float)P.C;
 #pragma unroll
-      for (int i = 0; i < UNITS; ++i)
+      for (int i = 0; i < U; ++i)
         if (tid + i * THREADS < units) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) y[i][e] -= mean;
@@ -115,67 +128,62 @@ __global__ void __launch_bounds__(THREADS == 32 ? kNormWarps * 32 : THREADS) k_n
     }
     float s = 0.0f;
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i)
+    for (int i = 0; i < U; ++i)
 #pragma unroll
       for (int e = 0; e < 8; ++e) s = fmaf(y[i][e], y[i][e], s);
     const float rstd = 1.0f / sqrtf(row_reduce<THREADS>(s, sh, add) / (float)P.C + P.eps);
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) {
+    for (int i = 0; i < U; ++i) {
       const int u = tid + i * THREADS;
-      if (u < units) {
-        float w[8];
-        if (P.weight != nullptr) load8<DT>(P.weight, u, w);
+      float g[8];
+      eight(w[i], g);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[i][e] *= P.weight != nullptr ? rstd * w[e] : rstd;
-        if (P.bias != nullptr) {
-          load8<DT>(P.bias, u, w);
+      for (int e = 0; e < 8; ++e) y[i][e] *= P.weight != nullptr ? rstd * g[e] : rstd;
+      if (P.bias != nullptr && u < units) {
+        load8<DT>(P.bias, u, g);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) y[i][e] += w[e];
-        }
+        for (int e = 0; e < 8; ++e) y[i][e] += g[e];
       }
     }
   }
   // The maximum of the magnitudes' bits, which order as the magnitudes do, infinities and NaN on top.
   uint32_t most = 0;
 #pragma unroll
-  for (int i = 0; i < UNITS; ++i)
+  for (int i = 0; i < U; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(y[i][e]) & 0x7FFFFFFFu);
-  most = __reduce_max_sync(0xFFFFFFFFu, most);
-  if constexpr (THREADS > 32)
-    most = __float_as_uint(row_reduce<THREADS>(__uint_as_float(most), sh, [](float a, float b) { return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b))); }));
+  most = __float_as_uint(row_reduce<THREADS>(__uint_as_float(most), sh, [](float a, float b) { return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b))); }));
   // A row with a value that is not finite gets a scale that is not a number, and products of it are none; a row of
   // nothing but (almost) zeros a scale of 0: below 2^-119, 127 / maximum has no fp32 value.
   const float amax = __uint_as_float(most);
   const bool finite = most < 0x7F800000u, some = finite && amax >= 1.504632769052528e-36f;
   const float inv = some ? 127.0f / amax : 0.0f;
 #pragma unroll
-  for (int i = 0; i < UNITS; ++i) {
+  for (int i = 0; i < U; ++i) {
     const int u = tid + i * THREADS;
-    if (u < units) {
+    if (in && u < units) {
       float z[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) z[e] = some ? fminf(fmaxf(y[i][e] * inv, -127.0f), 127.0f) : 0.0f;
       P.q[u0 + u] = make_uint2(pack_int8(z[0], z[1], z[2], z[3]), pack_int8(z[4], z[5], z[6], z[7]));
     }
   }
-  if (tid == 0) P.scale[row] = some ? amax / 127.0f : (finite ? 0.0f : __int_as_float(0x7FC00000));
+  if (tid == 0 && in) P.scale[row] = some ? amax / 127.0f : (finite ? 0.0f : __int_as_float(0x7FC00000));
 }
 
-constexpr int kNormMaxC = 256 * 8 * 8;
+constexpr int kNormMaxC = 512 * kNormUnits * 8;
 
 template <int DT>
 static inline cudaError_t norm_q8_launch(const NormQ8Args& P, cudaStream_t st) {
-  const int units = P.C / 8;
-  const auto warp_rows = [&](auto kernel) { return launch_dependent(kernel, dim3((P.rows + kNormWarps - 1) / kNormWarps), kNormWarps * 32, 1, 0, st, true, P); };
-  const auto cta_rows = [&](auto kernel, int threads) { return launch_dependent(kernel, dim3(P.rows), threads, 1, 0, st, true, P); };
-  if (units <= 32) return warp_rows(k_norm_q8<DT, 32, 1>);
-  if (units <= 64) return warp_rows(k_norm_q8<DT, 32, 2>);
-  if (units <= 128) return warp_rows(k_norm_q8<DT, 32, 4>);
-  if (units <= 256) return cta_rows(k_norm_q8<DT, 256, 1>, 256);
-  if (units <= 512) return cta_rows(k_norm_q8<DT, 256, 2>, 256);
-  if (units <= 1024) return cta_rows(k_norm_q8<DT, 256, 4>, 256);
-  return cta_rows(k_norm_q8<DT, 256, 8>, 256);
+  const int threads = (P.C / 8 + kNormUnits - 1) / kNormUnits;
+  const auto launch = [&](auto kernel, int t) { const int rows = norm_cta(t) / t; return launch_dependent(kernel, dim3((P.rows + rows - 1) / rows), norm_cta(t), 1, 0, st, true, P); };
+  if (threads <= 8) return launch(k_norm_q8<DT, 8>, 8);
+  if (threads <= 16) return launch(k_norm_q8<DT, 16>, 16);
+  if (threads <= 32) return launch(k_norm_q8<DT, 32>, 32);
+  if (threads <= 64) return launch(k_norm_q8<DT, 64>, 64);
+  if (threads <= 128) return launch(k_norm_q8<DT, 128>, 128);
+  if (threads <= 256) return launch(k_norm_q8<DT, 256>, 256);
+  return launch(k_norm_q8<DT, 512>, 512);
 }
 
 // ---------------------------------------------------------------- an 8-bit cache: rows in, rows out
