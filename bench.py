@@ -495,7 +495,7 @@ def run_stack(args) -> None:
     sampler = ClockSampler(uuid if uuid.startswith("GPU-") else "GPU-" + uuid)
     sampler.start()
     model = H.ProjectionStack(cfg, dev, matmul=args.scaffold) if args.config == "c3" else \
-        H.Aggregator(cfg, dev, matmul=args.scaffold, frame_attention=args.scaffold)
+        H.Aggregator(cfg, dev, matmul=args.scaffold, frame_attention="torch" if args.scaffold == "torch" else "library")
     stream = torch.cuda.current_stream()
     fill = -(-Bud // M) + 1
     pool = min(args.pool, 24)
@@ -575,7 +575,8 @@ def run_stack(args) -> None:
                                         "note": "events around every call of the streaming step's entry points in a "
                                                 f"separate pass of {n_split} frames; scaffold = projections, MLPs, "
                                                 "LayerNorm, frame attention with random-init weights "
-                                                f"(matmuls and frame attention on: {args.scaffold})"},
+                                                f"(matmuls and frame attention on: {args.scaffold}"
+                                                + ("; products of 8-bit rows)" if args.scaffold == "int8" else ")")},
             "e2e": None, "gpu_launches": int(launches), "launches_per_step": launches / K, "clocks": clocks,
             "roofline": {"kernel": "k_attn_tcgen05", "bound": "tensor", "achieved": achieved, "peak": peak,
                          "unit": "TFLOP/s", "frac": achieved / peak, "peak_kind": f"{peak_kind} burst cuBLAS bf16 peak",
@@ -703,8 +704,9 @@ def main():
     ap.add_argument("--impl", default="ours", choices=["ours", "reference", "launch-check"])
     ap.add_argument("--config", default="c2", choices=sorted(WORKLOADS))
     ap.add_argument("--compaction", default="fill", choices=["fill", "stable"])
-    ap.add_argument("--scaffold", default="library", choices=["library", "torch"],
-                    help="c3 / c4: projections, MLPs and frame attention on the library's tcgen05 kernels or on torch")
+    ap.add_argument("--scaffold", default="library", choices=["library", "int8", "torch"],
+                    help="c3 / c4: projections, MLPs and frame attention on the library's tcgen05 kernels (int8: its products of "
+                         "8-bit rows) or on torch")
     ap.add_argument("--streams", type=int, default=0, help="independent streams in rotation (0: enough to exceed L2)")
     ap.add_argument("--pool", type=int, default=160, help="distinct frames kept on the device (cycled beyond)")
     ap.add_argument("--e2e-steps", type=int, default=200)

@@ -394,7 +394,8 @@ int ovggt_k_linear_q8(const int8_t* A, const float* a_scale, const int8_t* W, co
  *
  * ovggt_k_store_q8: rows k, v [n_seqs, M, n_heads * 64] in dtype to rows start[s] .. start[s] + M - 1 of sequence s (start: device
  * [n_seqs], NULL = 0).  A sequence whose start is negative is left alone, and so is what would lie beyond the capacity.
- * ovggt_k_load_q8: rows first .. first + n - 1 of every sequence to k, v [n_seqs, n, n_heads * 64] in dtype. */
+ * ovggt_k_load_q8: rows first .. first + n - 1 of every sequence to k, v [n_seqs, n, n_heads * 64] in dtype; up to 65535 sequences and 2^27 rows
+ * times heads of each (OVGGT_ERR_UNSUPPORTED). */
 int ovggt_k_store_q8(const void* k, const void* v, int32_t n_seqs, int32_t M, int32_t n_heads, int32_t dtype, const int32_t* start,
                      int32_t capacity, int8_t* kq, uint8_t* kx, int8_t* vq, uint8_t* vx, void* stream);
 int ovggt_k_load_q8(const int8_t* kq, const uint8_t* kx, const int8_t* vq, const uint8_t* vx, int32_t n_seqs, int32_t n_heads,

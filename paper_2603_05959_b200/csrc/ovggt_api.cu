@@ -1676,11 +1676,12 @@ extern "C" int ovggt_k_load_q8(const int8_t* kq, const uint8_t* kx, const int8_t
     return OVGGT_ERR_INVALID_ARG;
   if (capacity % 16 != 0) return OVGGT_ERR_UNSUPPORTED;
   if (!aligned16(k) || !aligned16(v) || !aligned16(kq) || !aligned16(vq) || !aligned16(kx) || !aligned16(vx)) return OVGGT_ERR_MISALIGNED;
-  const long long ctas = ((long long)n_seqs * n * n_heads * 4 + 255) / 256;
-  if (ctas > 0x7FFFFFFF) return OVGGT_ERR_UNSUPPORTED;
-  const LoadQ8Args P = {{reinterpret_cast<const uint4*>(kq), reinterpret_cast<const uint4*>(vq)}, {kx, vx}, {k, v}, n_seqs, first, n, n_heads, capacity};
+  const int per_row = n_heads * (dtype == kBF16 ? 8 : 16);                    // 16-byte groups of output
+  if ((long long)n * n_heads * 16 > 0x7FFFFF00 || n_seqs > 65535) return OVGGT_ERR_UNSUPPORTED;
+  const LoadQ8Args P = {{kq, vq}, {kx, vx}, {k, v}, first, n, n_heads, capacity};
+  const dim3 grid((unsigned)(((long long)n * per_row + 256 * kLoadGroups - 1) / (256 * kLoadGroups)), n_seqs, 2);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  CK(launch_dependent(dtype == kBF16 ? k_load_q8<kBF16> : k_load_q8<kF32>, dim3((unsigned)ctas, 2), 256, 1, 0, st, true, P));
+  CK(launch_dependent(dtype == kBF16 ? k_load_q8<kBF16> : k_load_q8<kF32>, grid, 256, 1, 0, st, true, P));
   LAUNCHED();
   return OVGGT_OK;
 }

@@ -54,11 +54,12 @@ __device__ __forceinline__ float row_reduce(float x, float* sh, Op op) {
 
 // Four groups of eight elements a thread, whatever the row's width: 8 to 512 threads a row, several rows a CTA where they are less than
 // 128.  All loads, the weight's among them, are requested before the first reduction.  What bounds it is memory (10992 x 1024 bf16 with a
-// residual: 79 MB), of a single row the trip to it: with one to four groups a thread, a warp up to 1024 columns and a CTA beyond, and weights
-// read where they are needed, 60000 x 256 took 23.6 us, 10992 x 4096 30.7 and one row of 1024 3.5.
+// residual: 79 MB in 12.3 us, 6.4 TB/s), of a single row the trip to it: with one to four groups a thread, a warp up to 1024 columns and a CTA beyond, and weights
+// read where they are needed, 60000 x 256 took 23.6 us instead of 18.1, 4000 x 8192 59 instead of 40 and one row of 1024 3.5 instead of 2.4.
+// PLAIN: neither a residual nor a norm, in instances with registers for no more (10992 x 4096: 25.1 us, without them 29.8).
 constexpr int kNormUnits = 4;
 __host__ __device__ constexpr int norm_cta(int threads) { return threads < 128 ? (threads == 64 ? 64 : 128) : threads; }
-template <int DT, int THREADS>
+template <int DT, int THREADS, bool PLAIN>
 __global__ void __launch_bounds__(norm_cta(THREADS)) k_norm_q8(const NormQ8Args P) {
   __shared__ float sh[16];
   constexpr int U = kNormUnits, kWords = DT == kBF16 ? 1 : 2;                 // 16-byte words of a group
@@ -70,7 +71,8 @@ __global__ void __launch_bounds__(norm_cta(THREADS)) k_norm_q8(const NormQ8Args 
   const int units = P.C / 8;
   const size_t u0 = (size_t)row * units;
   const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-  uint4 x[U][kWords], r[U][kWords], w[U][kWords];
+  constexpr int V = PLAIN ? 1 : U;
+  uint4 x[U][kWords], r[V][kWords], w[V][kWords];
 #pragma unroll
   for (int i = 0; i < U; ++i)
 #pragma unroll
@@ -78,8 +80,10 @@ __global__ void __launch_bounds__(norm_cta(THREADS)) k_norm_q8(const NormQ8Args 
       const int u = tid + i * THREADS;
       const bool here = in && u < units;
       x[i][j] = here ? P.x[(u0 + u) * kWords + j] : zero;
-      r[i][j] = here && P.residual != nullptr ? P.residual[(u0 + u) * kWords + j] : zero;
-      w[i][j] = u < units && P.weight != nullptr ? P.weight[(size_t)u * kWords + j] : zero;
+      if constexpr (!PLAIN) {
+        r[i][j] = here && P.residual != nullptr ? P.residual[(u0 + u) * kWords + j] : zero;
+        w[i][j] = u < units && P.weight != nullptr ? P.weight[(size_t)u * kWords + j] : zero;
+      }
     }
   auto eight = [](const uint4 (&v)[kWords], float* f) {
     unpack<DT>(v[0], f);
@@ -89,9 +93,9 @@ __global__ void __launch_bounds__(norm_cta(THREADS)) k_norm_q8(const NormQ8Args 
 #pragma unroll
   for (int i = 0; i < U; ++i) {
     eight(x[i], y[i]);
-    if (P.residual != nullptr) {
+    if (!PLAIN && P.residual != nullptr) {
       float b[8];
-      eight(r[i], b);
+      eight(r[PLAIN ? 0 : i], b);
       uint4 s[kWords];
       if constexpr (DT == kBF16) {
         uint32_t* o = reinterpret_cast<uint32_t*>(s);
@@ -111,7 +115,7 @@ __global__ void __launch_bounds__(norm_cta(THREADS)) k_norm_q8(const NormQ8Args 
     }
   }
   const auto add = [](float a, float b) { return a + b; };
-  if (P.kind != OVGGT_NORM_NONE) {
+  if (!PLAIN && P.kind != OVGGT_NORM_NONE) {
     if (P.kind == OVGGT_NORM_LAYER) {
       float s = 0.0f;
 #pragma unroll
@@ -136,7 +140,7 @@ __global__ void __launch_bounds__(norm_cta(THREADS)) k_norm_q8(const NormQ8Args 
     for (int i = 0; i < U; ++i) {
       const int u = tid + i * THREADS;
       float g[8];
-      eight(w[i], g);
+      eight(w[PLAIN ? 0 : i], g);
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[i][e] *= P.weight != nullptr ? rstd * g[e] : rstd;
       if (P.bias != nullptr && u < units) {
@@ -176,14 +180,18 @@ constexpr int kNormMaxC = 512 * kNormUnits * 8;
 template <int DT>
 static inline cudaError_t norm_q8_launch(const NormQ8Args& P, cudaStream_t st) {
   const int threads = (P.C / 8 + kNormUnits - 1) / kNormUnits;
-  const auto launch = [&](auto kernel, int t) { const int rows = norm_cta(t) / t; return launch_dependent(kernel, dim3((P.rows + rows - 1) / rows), norm_cta(t), 1, 0, st, true, P); };
-  if (threads <= 8) return launch(k_norm_q8<DT, 8>, 8);
-  if (threads <= 16) return launch(k_norm_q8<DT, 16>, 16);
-  if (threads <= 32) return launch(k_norm_q8<DT, 32>, 32);
-  if (threads <= 64) return launch(k_norm_q8<DT, 64>, 64);
-  if (threads <= 128) return launch(k_norm_q8<DT, 128>, 128);
-  if (threads <= 256) return launch(k_norm_q8<DT, 256>, 256);
-  return launch(k_norm_q8<DT, 512>, 512);
+  const bool plain = P.kind == OVGGT_NORM_NONE && P.residual == nullptr;
+  const auto launch = [&](auto t) {
+    constexpr int T = decltype(t)::value, kRows = norm_cta(T) / T;
+    return launch_dependent(plain ? k_norm_q8<DT, T, true> : k_norm_q8<DT, T, false>, dim3((P.rows + kRows - 1) / kRows), norm_cta(T), 1, 0, st, true, P);
+  };
+  if (threads <= 8) return launch(std::integral_constant<int, 8>{});
+  if (threads <= 16) return launch(std::integral_constant<int, 16>{});
+  if (threads <= 32) return launch(std::integral_constant<int, 32>{});
+  if (threads <= 64) return launch(std::integral_constant<int, 64>{});
+  if (threads <= 128) return launch(std::integral_constant<int, 128>{});
+  if (threads <= 256) return launch(std::integral_constant<int, 256>{});
+  return launch(std::integral_constant<int, 512>{});
 }
 
 // ---------------------------------------------------------------- an 8-bit cache: rows in, rows out
@@ -235,10 +243,10 @@ __global__ void __launch_bounds__(256) k_store_q8(const StoreQ8Args P) {
 }
 
 struct LoadQ8Args {
-  const uint4* q[2];
+  const void* q[2];
   const uint8_t* x[2];
   void* dst[2];                        // [seqs, n, C]
-  int seqs, first, n, H, cap;
+  int first, n, H, cap;
 };
 
 // 2^(x - 133), the step of a block whose exponent byte is x; NaN for 255.
@@ -249,38 +257,55 @@ __device__ __forceinline__ float int8_at(uint32_t flipped) {   // (flipped: the 
   return __uint_as_float(__byte_perm(flipped, 0x4B000000u, 0x7440 + I)) - 8388736.0f;
 }
 
-// Sixteen elements a thread.
+// Bound by memory.  Whole lines both ways: four groups of 16 bytes of output a thread, a CTA's width apart; stores that leave L2 first, since what
+// is read back is as a rule larger than it.  17758 rows of 16 heads: bf16 18.1 us (6.0 TB/s), fp32 30.0; with ordinary stores 20.8 and 36.4, with
+// 16 elements a thread side by side 19.8 and 41.7, with eight groups a thread 21.3 and 31.0.
+constexpr int kLoadGroups = 4;
 template <int DT>
 __global__ void __launch_bounds__(256) k_load_q8(const LoadQ8Args P) {
+  constexpr int E = VecOf<DT>::n, kWords = E / 4;        // elements of a group, its words of int8
   pdl_trigger();
   pdl_wait();
-  const long long at = (long long)blockIdx.x * 256 + threadIdx.x, block = at >> 2;
-  const long long row = block / P.H;
-  if (row >= (long long)P.seqs * P.n) return;
-  const int h = (int)(block - row * P.H), seq = (int)(row / P.n), side = blockIdx.y;
-  const int from = P.first + (int)(row - (long long)seq * P.n);
-  const uint4 w = (side == 0 ? P.q[0] : P.q[1])[(((size_t)seq * P.cap + from) * P.H + h) * 4 + (at & 3)];
-  const float step = q8_step((side == 0 ? P.x[0] : P.x[1])[((size_t)seq * P.H + h) * P.cap + from]);
-  float f[16];
-  const uint32_t u[4] = {w.x ^ 0x80808080u, w.y ^ 0x80808080u, w.z ^ 0x80808080u, w.w ^ 0x80808080u};
+  const int seq = blockIdx.y, side = blockIdx.z;
+  const unsigned per_row = (unsigned)P.H * (64 / E), all = (unsigned)P.n * per_row, g0 = blockIdx.x * (256u * kLoadGroups) + threadIdx.x;
+  const uint32_t* q = reinterpret_cast<const uint32_t*>(side == 0 ? P.q[0] : P.q[1]) + ((size_t)seq * P.cap + P.first) * P.H * 16;
+  const uint8_t* xs = (side == 0 ? P.x[0] : P.x[1]) + (size_t)seq * P.H * P.cap + P.first;
+  uint4* d = static_cast<uint4*>(side == 0 ? P.dst[0] : P.dst[1]) + (size_t)seq * all;
+  uint32_t w[kLoadGroups][kWords], x[kLoadGroups];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    f[4 * i] = int8_at<0>(u[i]) * step;
-    f[4 * i + 1] = int8_at<1>(u[i]) * step;
-    f[4 * i + 2] = int8_at<2>(u[i]) * step;
-    f[4 * i + 3] = int8_at<3>(u[i]) * step;
+  for (int j = 0; j < kLoadGroups; ++j) {
+    const unsigned g = g0 + 256u * j;
+    if (g < all) {
+      if constexpr (kWords == 2) {
+        const uint2 v = *reinterpret_cast<const uint2*>(q + (size_t)g * 2);
+        w[j][0] = v.x, w[j][kWords - 1] = v.y;
+      } else {
+        w[j][0] = q[g];
+      }
+      const unsigned row = g / per_row;
+      x[j] = xs[(size_t)((g - row * per_row) / (64 / E)) * P.cap + row];
+    }
   }
-  if constexpr (DT == kBF16) {
-    uint32_t o[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = pack_bf16(f[2 * i], f[2 * i + 1]);
-    uint4* d = static_cast<uint4*>(side == 0 ? P.dst[0] : P.dst[1]) + 2 * (size_t)at;
-    d[0] = make_uint4(o[0], o[1], o[2], o[3]);
-    d[1] = make_uint4(o[4], o[5], o[6], o[7]);
-  } else {
-    float4* d = static_cast<float4*>(side == 0 ? P.dst[0] : P.dst[1]) + 4 * (size_t)at;
+  for (int j = 0; j < kLoadGroups; ++j) {
+    const unsigned g = g0 + 256u * j;
+    if (g < all) {
+      const float step = q8_step(x[j]);
+      float f[E];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) d[i] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+      for (int i = 0; i < kWords; ++i) {
+        const uint32_t u = w[j][i] ^ 0x80808080u;
+        f[4 * i] = int8_at<0>(u) * step;
+        f[4 * i + 1] = int8_at<1>(u) * step;
+        f[4 * i + 2] = int8_at<2>(u) * step;
+        f[4 * i + 3] = int8_at<3>(u) * step;
+      }
+      if constexpr (DT == kBF16) {
+        __stcs(d + g, make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[E - 4], f[E - 3]), pack_bf16(f[E - 2], f[E - 1])));
+      } else {
+        __stcs(d + g, make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])));
+      }
+    }
   }
 }
 

@@ -111,12 +111,15 @@ class _Timer:
 class _Scaffold:
     """The dense products of a workload and what surrounds them: on torch, or on the library's own kernels
     (ovggt_k_linear_bf16 with GELU, residual sum and the split of a QKV product in its epilogue; buffers that are kept
-    between frames; LayerNorm is torch's, which computes in fp32 and rounds once).  Both round to bf16 at the same places.  Either way it is scaffold time, not
-    the streaming step's."""
+    between frames; LayerNorm is torch's, which computes in fp32 and rounds once).  Both round to bf16 at the same places.
+    "int8": the library's products of 8-bit rows (ovggt_k_linear_q8): weights quantised once, a scale for each channel, and what they are
+    multiplied with as it comes, a scale for each token, behind its LayerNorm where there is one (ovggt_k_norm_q8).  Either way it is
+    scaffold time, not the streaming step's."""
 
     def __init__(self, kind: str, device):
-        assert kind in ("torch", "library")
+        assert kind in ("torch", "library", "int8")
         self.library = kind == "library"
+        self.int8 = kind == "int8"
         self.device = device
         self.status = torch.zeros(16, dtype=torch.int32, device=device)
         self._kept = {}
@@ -127,11 +130,30 @@ class _Scaffold:
             t = self._kept[name] = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
         return t
 
-    def layer_norm(self, x):
+    def weight(self, w):
+        """A weight [K, N] as the products below take it: itself, or its channels in 8 bits (rows [N, K] and their scales)."""
+        return B.k_norm_q8(w.T.contiguous(), kind=B.NORM_NONE) if self.int8 else w
+
+    def _rows(self, x, kind=B.NORM_NONE, stream=None):
+        """x in 8 bits, in buffers that are kept for rows of its shape: they are read by the product that follows."""
+        shape = tuple(x.shape)
+        q, scale = self._kept.get(shape) or self._kept.setdefault(shape, (torch.empty(shape, dtype=torch.int8, device=self.device),
+                                                                          torch.empty(shape[:1], dtype=torch.float32, device=self.device)))
+        return B.k_norm_q8(x, kind=kind, eps=1e-5, q=q, scale=scale, stream=stream)
+
+    def layer_norm(self, x, stream=None):
+        """LayerNorm of x for the product that follows."""
+        if self.int8:
+            return self._rows(x, B.NORM_LAYER, stream)
         return torch.nn.functional.layer_norm(x, (x.shape[-1],))
 
     def qkv(self, x, w, stream=None):
         """The three [M, C] column blocks of x W."""
+        if self.int8:
+            a, scale = x if isinstance(x, tuple) else self._rows(x, stream=stream)
+            out = [self.kept("qkv%d" % i, (a.shape[0], w[0].shape[0] // 3)) for i in range(3)]
+            B.k_linear_q8(a, scale, *w, out, status=self.status, stream=stream)
+            return out
         M, C = x.shape[0], w.shape[1] // 3
         if self.library:
             out = [self.kept("qkv%d" % i, (M, C)) for i in range(3)]
@@ -142,6 +164,11 @@ class _Scaffold:
 
     def add_product(self, x, a, w, out=None, product=None, stream=None):
         """x + a W, to `out` if given; the product itself to `product` if given."""
+        if self.int8:
+            out = torch.empty_like(x) if out is None else out
+            B.k_linear_q8(*self._rows(a, stream=stream), *w, () if product is None else (product,), residual=x, sum_out=out, status=self.status,
+                          stream=stream)
+            return out
         if self.library:
             out = torch.empty_like(x) if out is None else out
             B.k_linear_bf16(a, w, () if product is None else (product,), residual=x, sum_out=out, status=self.status,
@@ -153,6 +180,10 @@ class _Scaffold:
         return torch.add(x, y, out=out) if out is not None else x + y
 
     def gelu_product(self, x, w, stream=None):
+        if self.int8:
+            h = self.kept("hidden", (x[0].shape[0], w[0].shape[0]))
+            B.k_linear_q8(*x, *w, (h,), gelu=True, status=self.status, stream=stream)
+            return h
         if self.library:
             h = self.kept("hidden", (x.shape[0], w.shape[1]))
             B.k_linear_bf16(x, w, (h,), gelu=True, status=self.status, stream=stream)
@@ -187,8 +218,8 @@ class ProjectionStack:
         g = torch.Generator(device=device)
         g.manual_seed(cfg.seed)
         C, L = cfg.dim, cfg.n_layers
-        self.w_qkv = [_randn((C, 3 * C), 0.02, device, torch.bfloat16, g) for _ in range(L)]
-        self.w_o = [_randn((C, C), 0.02, device, torch.bfloat16, g) for _ in range(L)]
+        self.w_qkv = [self.mm.weight(_randn((C, 3 * C), 0.02, device, torch.bfloat16, g)) for _ in range(L)]
+        self.w_o = [self.mm.weight(_randn((C, C), 0.02, device, torch.bfloat16, g)) for _ in range(L)]
         self.out = self.cache.new_out()
         self.tap: Optional[Callable] = None
         self.after: Optional[Callable] = None
@@ -230,7 +261,7 @@ class Aggregator:
                  batched_compress: bool = True, frame_attention: str = "library", matmul: str = "library"):
         """frame_attention: "library" runs the attention among the frame's own tokens on the library's tcgen05 kernel
         (ovggt_k_attention with N = M: the same kernel that serves the cache); "torch" uses torch's SDPA.
-        matmul: "library" runs every projection and MLP product on ovggt_k_gemm_bf16; "torch" on torch's matmul."""
+        matmul: "library" runs every projection and MLP product on ovggt_k_linear_bf16, "int8" on ovggt_k_linear_q8; "torch" on torch's matmul."""
         self.batched_compress = batched_compress
         self.mm = _Scaffold(matmul, device)
         self.frame_attention = frame_attention
@@ -244,7 +275,7 @@ class Aggregator:
         g = torch.Generator(device=device)
         g.manual_seed(cfg.seed + 1)
         C, L, bf = cfg.dim, cfg.n_layers, torch.bfloat16
-        mk = lambda shape: _randn(shape, 0.02, device, bf, g)
+        mk = lambda shape: self.mm.weight(_randn(shape, 0.02, device, bf, g))
         self.blocks = [{kind: {"qkv": mk((C, 3 * C)), "o": mk((C, C)), "fc1": mk((C, 4 * C)), "fc2": mk((4 * C, C))}
                         for kind in ("frame", "global")} for _ in range(L)]
         self.out = self.cache.new_out()
@@ -260,7 +291,7 @@ class Aggregator:
         keep = (lambda name: mm.kept(name, (M, C)))
         for l in range(L):
             w = self.blocks[l]["frame"]
-            fq, fk, fv = mm.qkv(mm.layer_norm(x), w["qkv"], stream)
+            fq, fk, fv = mm.qkv(mm.layer_norm(x, stream), w["qkv"], stream)
             if self.frame_attention == "library":
                 a = B.k_attention(fq, fk, fv, H, out=self._fa_out, scratch=self._fa_scratch, status=self._fa_status,
                                   stream=stream)
@@ -268,10 +299,10 @@ class Aggregator:
                 q3 = [y.view(M, H, C // H).permute(1, 0, 2) for y in (fq, fk, fv)]               # [H, M, d]
                 a = torch.nn.functional.scaled_dot_product_attention(*q3).permute(1, 0, 2).reshape(M, C)
             x = mm.add_product(x, a, w["o"], out=keep("frame attended"), stream=stream)
-            x = mm.add_product(x, mm.gelu_product(mm.layer_norm(x), w["fc1"], stream), w["fc2"],
+            x = mm.add_product(x, mm.gelu_product(mm.layer_norm(x, stream), w["fc1"], stream), w["fc2"],
                                out=keep("frame out"), stream=stream)
             w = self.blocks[l]["global"]
-            q, k, v = mm.qkv(mm.layer_norm(x), w["qkv"], stream)
+            q, k, v = mm.qkv(mm.layer_norm(x, stream), w["qkv"], stream)
             att = lambda: self.cache.layer_attend(l, t, q, k, v, out=self.out, stream=stream)
             lib(att) if lib else att()
             if self.after:
@@ -280,7 +311,7 @@ class Aggregator:
             # the block's MLP output is the layer's residual, read by its compress: one buffer per layer
             r = keep("resid%d" % (l if self.batched_compress else 0))
             # (the frame's result is the caller's; what is passed between the layers is kept)
-            x = mm.add_product(h, mm.gelu_product(mm.layer_norm(h), w["fc1"], stream), w["fc2"],
+            x = mm.add_product(h, mm.gelu_product(mm.layer_norm(h, stream), w["fc1"], stream), w["fc2"],
                                out=None if l + 1 == L else keep("global out"), product=r, stream=stream)
             ov = self.tap(t, l, *_own(q, k, v, r)) if self.tap else None
             if self.batched_compress:
