@@ -565,7 +565,7 @@ __global__ void __launch_bounds__(256) k_widen_q8(const WidenArgs P) {
 #pragma unroll
   for (int j = 0; j < kWidenUnits; ++j) {
     const int u = threadIdx.x + 256 * j, i = u / units;
-    if (u < all) w[j] = ld_nc(src + (P.live != nullptr ? from[i] : i) * pitch + (u - i * units));
+    if (u < all) w[j] = __ldcg(src + (P.live != nullptr ? from[i] : i) * pitch + (u - i * units));
   }
   if ((int)threadIdx.x < units) {                        // (16 rows at a time: the capacity is a multiple of 16)
     const int h = threadIdx.x >> 2, r = (threadIdx.x & 3) * 16;

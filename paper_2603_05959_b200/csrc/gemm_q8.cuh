@@ -120,8 +120,8 @@ __global__ void __launch_bounds__(256) k_linear_q8_few(const GemmQ8Args P) {
 #pragma unroll 2
   for (int k = warp * 64 + 16 * t; k - 16 * t < K; k += 512) {
     const bool in = k < K;
-    const uint4 u = in && n0 + g < N ? ld_nc(reinterpret_cast<const uint4*>(w0 + k)) : zero;
-    const uint4 v = in && n0 + 8 + g < N ? ld_nc(reinterpret_cast<const uint4*>(w1 + k)) : zero;
+    const uint4 u = in && n0 + g < N ? __ldcg(reinterpret_cast<const uint4*>(w0 + k)) : zero;
+    const uint4 v = in && n0 + 8 + g < N ? __ldcg(reinterpret_cast<const uint4*>(w1 + k)) : zero;
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) {
       const int m = m0 + 8 * i + g;
@@ -187,6 +187,66 @@ __device__ __forceinline__ void mma_ss_s8(uint32_t d_tmem, uint64_t a_desc, uint
       " tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n}\n" ::"r"(d_tmem), "l"(a_desc), "l"(b_desc),
       "r"(idesc), "r"(acc)
       : "memory");
+}
+
+// A warp's 32 tokens (from row0) and quarter of a tile's channels (from col0): its sums from tensor memory (t_row) to where the caller wants
+// them, by way of its part of the staging; free() once the last of the sums has been read.
+template <int BN, bool GELU, bool RES, typename Free>
+__device__ __forceinline__ void q8_epilogue(const GemmQ8Args& P, uint32_t t_row, int row0, int col0, uint4* stage, Free free) {
+  constexpr int kCols = BN / 4, kChunk = q8_chunk(BN), kUnits = kChunk / 8;   // a warp's channels, those of a round, their 16-byte units
+  const int lane = threadIdx.x & 31;
+  const float as = row0 + lane < P.o.M ? P.a_scale[row0 + lane] : 0.0f;
+#pragma unroll 1
+  for (int c = 0; c < kCols; c += kChunk) {
+    const int col = col0 + c;
+    uint4 res[RES ? kUnits : 1];
+    if constexpr (RES) {
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) {
+        const int r = row0 + (lane + 32 * i) / kUnits, n = col + (lane + 32 * i) % kUnits * 8;
+        if (r < P.o.M && n < P.o.N) res[i] = *reinterpret_cast<const uint4*>(P.o.residual + (size_t)r * P.o.N + n);
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < kChunk; h += 16) {
+      uint32_t o[16];
+      float4 ws[4];
+      tmem_ld16(t_row + c + h, o);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {                      // (N a multiple of 8: scales past it are not read)
+        const int n = col + h + 4 * e;
+        ws[e] = n < P.o.N ? *reinterpret_cast<const float4*>(P.w_scale + n) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      tmem_wait_ld();
+      if (c + kChunk >= kCols && h + 16 >= kChunk) {     // the last of this tile's sums: the buffer is free
+        tc_fence_before();
+        if (lane == 0) free();
+      }
+      uint32_t w[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 x = mul2(mul2(make_float2((float)(int)o[4 * e], (float)(int)o[4 * e + 1]), make_float2(as, as)), make_float2(ws[e].x, ws[e].y));
+        const float2 y = mul2(mul2(make_float2((float)(int)o[4 * e + 2], (float)(int)o[4 * e + 3]), make_float2(as, as)), make_float2(ws[e].z, ws[e].w));
+        w[2 * e] = pack_bf16(x.x, x.y);
+        w[2 * e + 1] = pack_bf16(y.x, y.y);
+      }
+      if constexpr (GELU) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = gelu_near(w[e]);
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        stage[lane * kUnits + ((h / 8 + u) ^ (lane & (kUnits - 1)))] = make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+      const int r = (lane + 32 * i) / kUnits, u = (lane + 32 * i) % kUnits;
+      if (row0 + r < P.o.M && col + u * 8 < P.o.N)
+        q8_store8<RES>(P.o, row0 + r, col + u * 8, stage[r * kUnits + (u ^ (r & (kUnits - 1)))], res[RES ? i : 0]);
+    }
+    __syncwarp();
+  }
 }
 
 // GELU and the residual's sum in instances of their own.
@@ -290,64 +350,16 @@ k_linear_q8_tcgen05(const __grid_constant__ CUtensorMap tm_a, const __grid_const
     __syncwarp();
   } else {
     // ------------------------------------------------ epilogue
-    constexpr int kCols = BN / 4, kChunk = q8_chunk(BN), kUnits = kChunk / 8;     // a warp's channels, those of a round, their 16-byte units
     const int quad = warp & 3, side = warp >> 2;
-    uint4* stage = reinterpret_cast<uint4*>(staging) + warp * 32 * kUnits;
+    uint4* stage = reinterpret_cast<uint4*>(staging) + warp * 32 * (q8_chunk(BN) / 8);
     int j = 0;
     for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x, ++j) {
-      const int buf = j & 1, row0 = tile % tiles_m * 128 + quad * 32, col0 = tile / tiles_m * BN + side * kCols;
-      const float as = row0 + lane < P.o.M ? P.a_scale[row0 + lane] : 0.0f;
+      const int buf = j & 1;
       ok = __all_sync(0xFFFFFFFFu, mbar_wait(&B->acc_full[buf], (uint32_t)(j / 2) & 1u, B, P.o.status)) != 0;
       if (!ok) break;
       tc_fence_after();
-      const uint32_t t_row = tmem + ((uint32_t)(quad * 32) << 16) + buf * BN + side * kCols;
-#pragma unroll 1
-      for (int c = 0; c < kCols; c += kChunk) {
-        const int col = col0 + c;
-        uint4 res[RES ? kUnits : 1];
-        if constexpr (RES) {
-#pragma unroll
-          for (int i = 0; i < kUnits; ++i) {
-            const int r = row0 + (lane + 32 * i) / kUnits, n = col + (lane + 32 * i) % kUnits * 8;
-            if (r < P.o.M && n < P.o.N) res[i] = *reinterpret_cast<const uint4*>(P.o.residual + (size_t)r * P.o.N + n);
-          }
-        }
-#pragma unroll
-        for (int h = 0; h < kChunk; h += 16) {
-          uint32_t o[16];
-          tmem_ld16(t_row + c + h, o);
-          tmem_wait_ld();
-          if (c + kChunk >= kCols && h + 16 >= kChunk) {                      // the last of this tile's sums: the buffer is free
-            tc_fence_before();
-            if (lane == 0) mbar_arrive(&B->acc_empty[buf]);
-          }
-          uint32_t w[8];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {                                        // (N a multiple of 8: scales past it are not read)
-            const int n = col + h + 4 * e;
-            const float4 ws = n < P.o.N ? __ldg(reinterpret_cast<const float4*>(P.w_scale + n)) : make_float4(0.f, 0.f, 0.f, 0.f);
-            const float2 x = mul2(mul2(make_float2((float)(int)o[4 * e], (float)(int)o[4 * e + 1]), make_float2(as, as)), make_float2(ws.x, ws.y));
-            const float2 y = mul2(mul2(make_float2((float)(int)o[4 * e + 2], (float)(int)o[4 * e + 3]), make_float2(as, as)), make_float2(ws.z, ws.w));
-            w[2 * e] = pack_bf16(x.x, x.y);
-            w[2 * e + 1] = pack_bf16(y.x, y.y);
-          }
-          if constexpr (GELU) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = gelu_near(w[e]);
-          }
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-            stage[lane * kUnits + ((h / 8 + u) ^ (lane & (kUnits - 1)))] = make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
-        }
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < kUnits; ++i) {
-          const int r = (lane + 32 * i) / kUnits, u = (lane + 32 * i) % kUnits;
-          if (row0 + r < P.o.M && col + u * 8 < P.o.N)
-            q8_store8<RES>(P.o, row0 + r, col + u * 8, stage[r * kUnits + (u ^ (r & (kUnits - 1)))], res[RES ? i : 0]);
-        }
-        __syncwarp();
-      }
+      q8_epilogue<BN, GELU, RES>(P, tmem + ((uint32_t)(quad * 32) << 16) + buf * BN + side * (BN / 4), tile % tiles_m * 128 + quad * 32,
+                                 tile / tiles_m * BN + side * (BN / 4), stage, [&]() { mbar_arrive(&B->acc_empty[buf]); });
     }
   }
 
