@@ -60,7 +60,7 @@ __device__ __forceinline__ uint32_t int8_to_bf16x2(uint32_t x) { return sub_bf16
 //   scores  by int8 MMAs on the cached bytes as they are.  A row of Q is taken as whole numbers of 15 bits, q = 2^(e - 13) (256 hi + lo), two int8
 //           operands: exact for elements down to 2^-6 of the row's largest, to 2^-14 of it for the rest.  With at
 //           most 8 rows hi and lo are the two halves of one operand of 16 rows.
-//   P V     with at most 8 rows by int8 MMAs too: a weight p 2^(x - 133) as a whole number of 31 bits, 2^-23 of a reference that follows the largest
+//   P V     with at most 8 rows by int8 MMAs too: a weight p 2^(x - 133) as a whole number of 31 bits, 2^-28 of a reference that follows the largest
 //           weight, four unsigned bytes in the halves of two operands; the cached bytes of four rows are only put side by side.  The int32 sums
 //           are exact and go into fp32 when the reference moves.  With more rows, where that many sums do not fit the registers, by bf16 MMAs: the
 //           cached bytes are exact in bf16, a weight is rounded to it (2^-8).  (One row over 32768, 16 heads: 17 us, by bf16 MMAs 22.)
@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(few_warps(ROWS) * 32, 1) k_attn_q8_few(const A
     }
     since = 0;
   };
-  constexpr float kUnits = 23.0f, kRoom = 8.0f;          // a reference weight is 2^23 units; another is at most 2^8 of it
+  constexpr float kUnits = 28.0f, kRoom = 3.0f;          // a reference weight is 2^28 units; another is at most 2^3 of it
   constexpr int kSumsMost = 2000;                        // tiles: 64000 x 255 x 127 is below 2^31
 #pragma unroll
   for (int i = 0; i < T; ++i) {
@@ -408,7 +408,7 @@ __global__ void __launch_bounds__(few_warps(ROWS) * 32, 1) k_attn_q8_few(const A
 
   // ---- a warp's result into its stages: O [ROWS][64], the maxima, the sums
   float* mine = reinterpret_cast<float*>(stages);
-  if constexpr (PACK) take_sums(mv == -INFINITY ? 0.0f : ex2(mv - (m[0][0] == -INFINITY ? mv : m[0][0])) * 1.1920928955078125e-07f);   // (2^-23)
+  if constexpr (PACK) take_sums(mv == -INFINITY ? 0.0f : ex2(mv - (m[0][0] == -INFINITY ? mv : m[0][0])) * 3.725290298461914e-09f);   // (2^-28)
 #pragma unroll
   for (int i = 0; i < T; ++i)
 #pragma unroll

@@ -48,7 +48,7 @@ def test_linear(lib):
                  dict(n_outs=4), dict(n_outs=-1), dict(outs=None), dict(residual=None), dict(sum=None), dict(n_outs=0, residual=None, sum=None),
                  dict(outs=(C.c_void_p * 3)(P, None, P))):
         assert call(**over) == BAD, over
-    for over in (dict(K=72), dict(N=28, n_outs=1), dict(N=32), dict(n_outs=2), dict(K=131072)):
+    for over in (dict(K=72), dict(N=28, n_outs=1), dict(N=32), dict(n_outs=2), dict(K=131072), dict(M=0x7FFFFF01), dict(N=0x7FFFFFF8, n_outs=1)):
         assert call(**over) == UNSUPPORTED, over
     for name in ("A", "W", "w_scale", "residual", "sum"):
         assert call(**{name: P + 8}) == MISALIGNED, name

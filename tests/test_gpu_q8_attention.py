@@ -157,6 +157,18 @@ def test_weights_that_grow_from_tile_to_tile(M):
         _check(q, cache)
 
 
+@pytest.mark.parametrize("M,capacity", [(1, 416), (8, 1008), (20, 416)] + ROWS_BY_PLANES)
+def test_one_row_of_large_values(M, capacity):
+    """One row's values are 2^14 times the others', in half the columns: the other half holds its zeros, and there the others are the result."""
+    q, cache = _case(1, M, 1, 1, capacity)
+    k, v = B.k_load_q8(cache, capacity, dtype=torch.float32)
+    v = v.sign() * (1 + v.abs() % 1)
+    v[0, capacity // 3] *= 2.0 ** 14
+    v[0, capacity // 3, 1::2] = 0
+    B.k_store_q8(cache, k, v)
+    _check(q, cache)
+
+
 @pytest.mark.parametrize("M,capacity", [(1, 224), (20, 224), (150, 224)] + ROWS_BY_PLANES)
 def test_what_lies_in_masked_places(M, capacity):
     """NaN blocks and bytes that no store wrote, beyond the length and under the mask, change nothing."""
