@@ -158,10 +158,13 @@ __global__ void __launch_bounds__(256) k_linear_q8_few(const GemmQ8Args P) {
 // A persistent CTA per SM takes tiles of 128 tokens x BN channels (256, 128 or 64) in turn.  K in steps of 128: A [128, 128] and W [BN, 128], both
 // K-major in 128-byte swizzled rows as they lie in memory, 32 columns of K an MMA, int32 sums in BN of 2 BN TMEM columns: while the epilogue
 // warps take one tile's sums, the MMAs of the next tile run.
-//   warps 0-15  epilogue: 32 tokens and a quarter of the channels each, 32 channels (64 or 128 wide tiles: 16 or 32) at a time, through 2 KB of
-//               shared memory into whole sectors
+//   warps 0-15  epilogue: 32 tokens and a quarter of the channels each, 32 channels (of 64 wide tiles 16) at a time, through 2 KB of shared memory
+//               (of 64 wide tiles 1) into whole sectors, by a bulk copy where a block of 32 channels has one output and no residual
 //   warp 16     TMA producer; warp 17 allocates tensor memory and issues the MMAs
-// Every wait is bounded, as in the bf16 product.
+// Every wait is bounded, as in the bf16 product.  Measured: 10992 x 4096 x 1024 42 us, 2200 TOPS (with GELU 48), 10992 x 1024 x 4096 with a residual 47,
+// 1041 x 4096 x 1024 with GELU 9.1, 1041 x 1024 x 4096 with a residual 10.8, 8192^3 391 (2810 TOPS).  The main loop alone runs at 3300 TOPS; what
+// bounds the first is the epilogue beside it: its arithmetic, and results that share L2 with the 48 KB a step that tiles take in (by the
+// threads' own stores 43 and 51 us).
 constexpr int kQ8K = 128, kQ8ATile = 128 * kQ8K;
 __host__ __device__ constexpr int q8_stage_bytes(int bn) { return kQ8ATile + bn * kQ8K; }
 __host__ __device__ constexpr int q8_stages(int bn) { return bn == 256 ? 4 : (bn == 128 ? 6 : 8); }
@@ -191,8 +194,8 @@ __device__ __forceinline__ void mma_ss_s8(uint32_t d_tmem, uint64_t a_desc, uint
 
 // A warp's 32 tokens (from row0) and quarter of a tile's channels (from col0): its sums from tensor memory (t_row) to where the caller wants
 // them, by way of its part of the staging; free() once the last of the sums has been read.
-template <int BN, bool GELU, bool RES, typename Free>
-__device__ __forceinline__ void q8_epilogue(const GemmQ8Args& P, uint32_t t_row, int row0, int col0, uint4* stage, Free free) {
+template <int BN, bool GELU, bool RES, bool BULK, typename Free>
+__device__ __forceinline__ void q8_epilogue(const GemmQ8Args& P, const CUtensorMap* out, uint32_t t_row, int row0, int col0, uint4* stage, Free free) {
   constexpr int kCols = BN / 4, kChunk = q8_chunk(BN), kUnits = kChunk / 8;   // a warp's channels, those of a round, their 16-byte units
   const int lane = threadIdx.x & 31;
   const float as = row0 + lane < P.o.M ? P.a_scale[row0 + lane] : 0.0f;
@@ -212,6 +215,11 @@ __device__ __forceinline__ void q8_epilogue(const GemmQ8Args& P, uint32_t t_row,
       uint32_t o[16];
       float4 ws[4];
       tmem_ld16(t_row + c + h, o);
+      if constexpr (BULK)
+        if (h == 0) {                                    // the staging's last contents have been read
+          asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+          __syncwarp();
+        }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {                      // (N a multiple of 8: scales past it are not read)
         const int n = col + h + 4 * e;
@@ -236,7 +244,19 @@ __device__ __forceinline__ void q8_epilogue(const GemmQ8Args& P, uint32_t t_row,
       }
 #pragma unroll
       for (int u = 0; u < 2; ++u)
-        stage[lane * kUnits + ((h / 8 + u) ^ (lane & (kUnits - 1)))] = make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
+        stage[lane * kUnits + ((h / 8 + u) ^ (BULK ? lane >> 1 & 3 : lane & (kUnits - 1)))] = make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
+    }
+    if constexpr (BULK) {                                // (rows and columns past the last are not written)
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0 && row0 < P.o.M && col < P.o.N) {
+        const int i = (col >= P.o.part) + ((unsigned)col >= 2u * (unsigned)P.o.part);
+        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(out + i), "r"(col - i * P.o.part), "r"(row0),
+                     "r"(smem_u32(stage))
+                     : "memory");
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+      }
+      continue;
     }
     __syncwarp();
 #pragma unroll
@@ -250,9 +270,11 @@ __device__ __forceinline__ void q8_epilogue(const GemmQ8Args& P, uint32_t t_row,
 }
 
 // GELU and the residual's sum in instances of their own.
-template <int BN, bool GELU, bool RES>
+struct OutMaps { CUtensorMap m[3]; };
+template <int BN, bool GELU, bool RES, bool BULK>
 __global__ void __launch_bounds__(kGemmThreads, 1)
-k_linear_q8_tcgen05(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ GemmQ8Args P) {
+k_linear_q8_tcgen05(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ OutMaps tm_out,
+                    const __grid_constant__ GemmQ8Args P) {
   constexpr int kStages = q8_stages(BN), kStage = q8_stage_bytes(BN);
   constexpr int kProducer = kGemmEpilogueWarps, kIssuer = kGemmEpilogueWarps + 1;
   extern __shared__ __align__(1024) unsigned char smem[];
@@ -358,9 +380,10 @@ k_linear_q8_tcgen05(const __grid_constant__ CUtensorMap tm_a, const __grid_const
       ok = __all_sync(0xFFFFFFFFu, mbar_wait(&B->acc_full[buf], (uint32_t)(j / 2) & 1u, B, P.o.status)) != 0;
       if (!ok) break;
       tc_fence_after();
-      q8_epilogue<BN, GELU, RES>(P, tmem + ((uint32_t)(quad * 32) << 16) + buf * BN + side * (BN / 4), tile % tiles_m * 128 + quad * 32,
+      q8_epilogue<BN, GELU, RES, BULK>(P, tm_out.m, tmem + ((uint32_t)(quad * 32) << 16) + buf * BN + side * (BN / 4), tile % tiles_m * 128 + quad * 32,
                                  tile / tiles_m * BN + side * (BN / 4), stage, [&]() { mbar_arrive(&B->acc_empty[buf]); });
     }
+    if (BULK && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");   // (written before the CTA ends)
   }
 
   tc_fence_before();
@@ -369,6 +392,21 @@ k_linear_q8_tcgen05(const __grid_constant__ CUtensorMap tm_a, const __grid_const
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)(2 * BN)) : "memory");
   }
+}
+
+// [rows, C] bf16 row-major; box = 32 columns x 32 rows, 64-byte swizzle.
+static inline int make_out_map(CUtensorMap* map, const void* base, int rows, int C) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) return OVGGT_ERR_CUDA;
+  cuuint64_t dims[2] = {(cuuint64_t)C, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)C * 2};
+  cuuint32_t box[2] = {32, 32}, estr[2] = {1, 1};
+  const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    g_attn_last_error = (int)r;
+    return OVGGT_ERR_CUDA;
+  }
+  return OVGGT_OK;
 }
 
 template <int BN>
@@ -380,13 +418,24 @@ static inline int q8_tcgen05_launch(const GemmQ8Args& P, cudaStream_t st) {
   rc = make_rows_map(&tw, P.w, P.o.N, P.o.K / 2, BN);
   if (rc) return rc;
   const bool gelu = P.o.gelu != 0, res = P.o.residual != nullptr;
-  const auto kernel = gelu ? (res ? k_linear_q8_tcgen05<BN, true, true> : k_linear_q8_tcgen05<BN, true, false>)
-                           : (res ? k_linear_q8_tcgen05<BN, false, true> : k_linear_q8_tcgen05<BN, false, false>);
-  static std::atomic<uint64_t> smem_set[4];
-  cudaError_t e = allow_smem(kernel, q8_smem_bytes(BN), smem_set[2 * gelu + res]);
+  // results by bulk copies where no block of 32 channels lies in two of the outputs
+  bool bulk = false;
+  OutMaps out = {};
+  auto kernel = gelu ? (res ? k_linear_q8_tcgen05<BN, true, true, false> : k_linear_q8_tcgen05<BN, true, false, false>)
+                     : (res ? k_linear_q8_tcgen05<BN, false, true, false> : k_linear_q8_tcgen05<BN, false, false, false>);
+  if constexpr (BN >= 128) {
+    bulk = !res && (P.o.part == P.o.N || P.o.part % 32 == 0);
+    if (bulk) kernel = gelu ? k_linear_q8_tcgen05<BN, true, false, true> : k_linear_q8_tcgen05<BN, false, false, true>;
+    for (int i = 0; bulk && i < 3 && P.o.out[i] != nullptr; ++i) {
+      rc = make_out_map(&out.m[i], P.o.out[i], P.o.M, P.o.part);
+      if (rc) return rc;
+    }
+  }
+  static std::atomic<uint64_t> smem_set[6];
+  cudaError_t e = allow_smem(kernel, q8_smem_bytes(BN), smem_set[bulk ? 4 + gelu : 2 * gelu + res]);
   const long tiles = (long)((P.o.M + 127) / 128) * ((P.o.N + BN - 1) / BN);
   if (tiles > 0x7FFF0000) return OVGGT_ERR_UNSUPPORTED;
-  if (e == cudaSuccess) e = launch_dependent(kernel, dim3((unsigned)std::min(tiles, 148l)), kGemmThreads, 1, q8_smem_bytes(BN), st, true, ta, tw, P);
+  if (e == cudaSuccess) e = launch_dependent(kernel, dim3((unsigned)std::min(tiles, 148l)), kGemmThreads, 1, q8_smem_bytes(BN), st, true, ta, tw, out, P);
   if (e != cudaSuccess) { g_attn_last_error = (int)e; return OVGGT_ERR_CUDA; }
   return OVGGT_OK;
 }

@@ -111,6 +111,20 @@ def test_rows_behind_the_last_are_left_alone(M):
     assert torch.equal(whole[:M], _t(a, as_, w, ws)) and bool((whole[M:] == 7).all())
 
 
+@pytest.mark.parametrize("M,N,parts,gelu", [(4499, 1032, 1, True), (2049, 2400, 3, False), (1375, 4096, 2, True), (20001, 264, 1, False)])
+def test_wide_tiles_write_their_rows_and_columns_alone(M, N, parts, gelu):
+    """Results that leave by bulk copies: nothing behind the last row of any of them, nothing of one in another."""
+    a, as_, w, ws, _, st = _case(M, N, 144)
+    whole = [torch.full((M + 130, N // parts), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(parts)]
+    B.k_linear_q8(a, as_, w, ws, [o[:M] for o in whole], gelu=gelu, status=st)
+    got, ref = torch.cat([o[:M] for o in whole], 1), _t(a, as_, w, ws)
+    if gelu:
+        _check_gelu(got, ref)
+    else:
+        assert torch.equal(got, ref)
+    assert all(bool((o[M:] == 7).all()) for o in whole) and int(st[0]) == 0
+
+
 def test_arguments():
     a, as_, w, ws, x, st = _case(16, 32, 64)
     t = torch.empty_like(x)
