@@ -63,11 +63,12 @@ __device__ __forceinline__ uint32_t int8_to_bf16x2(uint32_t x) { return sub_bf16
 //   P V     with at most 8 rows by int8 MMAs too: a weight p 2^(x - 133) as a whole number of 31 bits, 2^-28 of a reference that follows the largest
 //           weight, four unsigned bytes in the halves of two operands; the cached bytes of four rows are only put side by side.  The int32 sums
 //           are exact and go into fp32 when the reference moves.  With more rows, where that many sums do not fit the registers, by bf16 MMAs: the
-//           cached bytes are exact in bf16, a weight is rounded to it (2^-8).  (One row over 32768, 16 heads: 17 us, by bf16 MMAs 22.)
+//           cached bytes are exact in bf16, a weight is rounded to it (2^-8).  (One row over 32768, 16 heads: 18 us, by bf16 MMAs 22.)
 // Which cached row or column an operand's row or column stands for is free, so each lane takes 16 bytes of a K row and 8
 // bytes of a V row at once.
-// A CTA has an SM to itself, and as many warps as its registers leave (8 rows by 16 warps, which spill: 28 us where 12 take 25, four tokens over 16384 rows).
-__host__ __device__ constexpr int few_warps(int rows) { return rows == 8 ? 12 : (rows == 16 ? 16 : 8); }
+// A CTA has an SM to itself, and as many warps as its registers leave without spilling (four tokens over up to 16384 rows by 16 warps 28 us, by 12
+// 25; 16 rows over 2048 8.6 and 7.9; 32 rows over 8192 by 12 warps 16.5, by 8 13.7).
+__host__ __device__ constexpr int few_warps(int rows) { return rows == 32 ? 8 : 12; }
 constexpr int kFewStages = 3, kFewKeys = 32;
 constexpr int kFewX = 2 * kFewKeys * 64;                 // of a stage: K, V, then the exponents of K and V and the mask, 32 bytes each
 constexpr int kFewStage = kFewX + 128;
