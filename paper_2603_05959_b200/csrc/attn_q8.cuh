@@ -54,7 +54,8 @@ __device__ __forceinline__ uint32_t int8_to_bf16x2(uint32_t x) { return sub_bf16
 
 // ---------------------------------------------------------------- few rows: the cache streams through, once per 8, 16 or 32 rows
 //
-// Bound by the cache's bytes.  A warp takes tiles of 32 cached rows by itself, with three of them on their way in its own stages
+// What bounds it: the cache's bytes (the copies alone take 10 of 18 us of one row over 32768), and beside them the arithmetic on them, chains of
+// copy, MMA, exponentials and MMA that a dozen warps an SM do not cover.  A warp takes tiles of 32 cached rows by itself, with three of them on their way in its own stages
 // (no barrier in the loop); the warps' results are joined through shared memory, those of the CTAs that share a sequence and head (parts) by
 // the bf16 attention's merge kernel.
 //   scores  by int8 MMAs on the cached bytes as they are.  A row of Q is taken as whole numbers of 15 bits, q = 2^(e - 13) (256 hi + lo), two int8
