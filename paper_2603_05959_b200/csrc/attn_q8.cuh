@@ -464,9 +464,9 @@ __global__ void __launch_bounds__(few_warps(ROWS) * 32, 1) k_attn_q8_few(const A
 
 // ---------------------------------------------------------------- many rows: tcgen05 over bf16 planes
 //
-// From two tiles of queries or so on, widening the cache once, into bf16 planes in scratch memory, costs less than each tile's doing it: a
-// plane takes 2.5 instructions an element and 5 bytes of traffic, most of it in L2 (17758 rows of 16 heads: 18 us beside 120 of
-// attention for 11 tiles of queries; widened on the way into shared memory, once for two tiles, the same attention took 250 us: the
+// From some tiles of queries on (see attn_q8_by_planes), widening the cache once, into bf16 planes in scratch memory, costs less than each tile's
+// doing it: a plane takes some 3 instructions an element and 5 bytes of traffic, most of it in L2 (17758 rows of 16 heads: 22 us beside 128 of
+// attention and merge for 11 tiles of queries; widened on the way into shared memory, once for two tiles, the same attention took 250 us: the
 // widening warps share the issue slots with the softmax).  The planes are what the cache stands for: q 2^(x - 133) is exact in bf16.
 constexpr size_t kPlanesAtOnce = (size_t)128 << 20;      // bytes of planes up to which sequences are taken together: what stays in L2
 constexpr size_t kPlanesMost = (size_t)2 << 30;          // beyond which the few-row kernel takes any number of rows
