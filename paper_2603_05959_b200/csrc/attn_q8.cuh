@@ -67,21 +67,20 @@ __device__ __forceinline__ uint32_t int8_to_bf16x2(uint32_t x) { return sub_bf16
 //           cached bytes are exact in bf16, a weight is rounded to it (2^-8).  (One row over 32768, 16 heads: 18 us, by bf16 MMAs 22.)
 // Which cached row or column an operand's row or column stands for is free, so each lane takes 16 bytes of a K row and 8
 // bytes of a V row at once.
-// A CTA has an SM to itself, and as many warps as its registers leave without spilling (four tokens over up to 16384 rows by 16 warps 28 us, by 12
-// 25; 16 rows over 2048 8.6 and 7.9; 32 rows over 8192 by 12 warps 16.5, by 8 13.7).
+// An SM holds as many warps as their registers leave without spilling (four tokens over up to 16384 rows by 16 warps 28 us, by 12 25; 16 rows
+// over 2048 8.6 and 7.9; 32 rows over 8192 by 12 warps 16.5, by 8 13.7), in one CTA or in two or three smaller ones (see attn_q8_plan).
 __host__ __device__ constexpr int few_warps(int rows) { return rows == 32 ? 8 : 12; }
 constexpr int kFewStages = 3, kFewKeys = 32;
 constexpr int kFewX = 2 * kFewKeys * 64;                 // of a stage: K, V, then the exponents of K and V and the mask, 32 bytes each
 constexpr int kFewStage = kFewX + 128;
 constexpr int kFewTable = kFewKeys * 16;                 // of a warp: (step of K, 0 or -inf under the mask, step of V) for each row of its tile
-__host__ __device__ constexpr int few_smem_bytes(int rows) {
-  return few_warps(rows) * (kFewStages * kFewStage + kFewTable) + (rows == 8 ? 1 : rows / 8) * 1024 + rows * 8;
+__host__ __device__ constexpr int few_smem_bytes(int rows, int warps) {
+  return warps * (kFewStages * kFewStage + kFewTable) + (rows == 8 ? 1 : rows / 8) * 1024 + rows * 8;
 }
 static_assert(kFewStages * kFewStage >= 32 * (64 + 2) * 4, "a warp's result does not fit its stages");
 
-template <int ROWS>
-__global__ void __launch_bounds__(few_warps(ROWS) * 32, 1) k_attn_q8_few(const AttnQ8Args P) {
-  constexpr int kFewWarps = few_warps(ROWS);
+template <int ROWS, int kFewWarps>
+__global__ void __launch_bounds__(kFewWarps * 32, few_warps(ROWS) / kFewWarps) k_attn_q8_few(const AttnQ8Args P) {
   constexpr bool PACK = ROWS == 8;
   constexpr int T = PACK ? 1 : ROWS / 16;                // operands of 16 rows
   constexpr int R = PACK ? 1 : 2;                        // rows of an operand a thread holds scores of
@@ -1030,9 +1029,9 @@ inline bool attn_q8_by_planes(long long cached, long long rows) {      // cached
   return 5e6 + 45.0 * x * (double)((rows + 31) / 32) > 11e6 + x * (118.0 + 25.0 * (double)((rows - 1) / kBM));
 }
 
-// How a call is cut: rows a CTA takes (8, 16, 32: the few-row kernel; 128), parts of the cached rows, sequences at once.
+// How a call is cut: rows a CTA takes (8, 16, 32: the few-row kernel, by so many warps; 128), parts of the cached rows, sequences at once.
 struct AttnQ8Plan {
-  int tile, q_tiles, parts, seqs, plane_rows;
+  int tile, warps, q_tiles, parts, seqs, plane_rows;
   size_t planes, o_part, ml_part, bytes;   // of scratch: K and V planes, the parts' results, where the live rows go and the norms; all
 };
 inline AttnQ8Plan attn_q8_plan(int seqs, int M, int H, int HK, int cap) {
@@ -1057,9 +1056,21 @@ inline AttnQ8Plan attn_q8_plan(int seqs, int M, int H, int HK, int cap) {
     A.tile = rows <= 8 ? 8 : (rows <= 16 ? 16 : 32);
     A.seqs = seqs;
     A.q_tiles = (int)((rows + A.tile - 1) / A.tile);
-    // as many CTAs as there are SMs, while each warp has a tile to take
-    const long long jobs = (long long)seqs * HK * A.q_tiles, places = 148, most = cap / (few_warps(A.tile) * kFewKeys);
-    A.parts = (int)std::max(1ll, std::min({(long long)kMaxSplits, places / jobs, most}));
+    // Warps a CTA and parts, by a model of the time in 10 ns: waves of CTAs over 148 SMs, each as long as a warp's tiles of 32 cached rows (a last
+    // one shorter, which has the SMs to itself) and its set-up and end, which smaller CTAs hide under one another's work, and a merge.  Fitted to 16 to 1024 sequences times heads over 256 to 32768 rows: 16 x
+    // 32768 by 12 warps 18 us, by 6 19, by 4 24; 80 x 8192 24, 19 and 17; 256 x 2048 20, 15.5 and 20; 1024 x 2048 66, 51 and 47.
+    const long long jobs = (long long)seqs * HK * A.q_tiles, tiles = (cap + kFewKeys - 1) / kFewKeys;
+    const int whole = few_warps(A.tile), step = A.tile == 8 ? 115 : (A.tile == 16 ? 168 : 157);
+    long long best = -1;
+    for (int per_sm = 1; per_sm <= (whole == 12 ? 3 : 2); ++per_sm)
+      for (int parts = 1; parts <= kMaxSplits; ++parts) {
+        const int warps = whole / per_sm, ends = per_sm == 1 ? 230 : (per_sm == 2 ? 130 : 90);
+        if (parts > 1 && (long long)(parts - 1) * warps >= tiles) break;       // (each part's first warp has a tile)
+        const long long places = 148 * per_sm, full = jobs * parts / places, rest = jobs * parts % places;
+        const long long a_warp = (tiles + (long long)parts * warps - 1) / ((long long)parts * warps) * step;
+        const long long cost = full * (a_warp + ends) + (rest ? a_warp * std::max(places * (full ? 45 : 90) / 100, rest) / places + ends : 0) + (parts > 1 ? 200 + 20 * parts : 0);
+        if (best < 0 || cost < best) best = cost, A.parts = parts, A.warps = warps;
+      }
   }
   A.o_part = A.parts == 1 ? 0 : (size_t)A.parts * A.seqs * M * H * kHD * 4;
   A.ml_part = A.parts == 1 ? 0 : (size_t)A.parts * A.seqs * M * H * 8;
@@ -1106,10 +1117,15 @@ static inline int attn_q8_launch(AttnQ8Args P, void* scratch, cudaStream_t st, i
       if (e == cudaSuccess) e = launch_dependent(k_attn_q8_many, dim3((unsigned)ctas), kAttnThreads, 1, kManySmem, st, true, tk, tv, P, (const int*)counts, (const unsigned*)norms, A.plane_rows);
       *launches += 2;
     } else {
-      const auto kernel = A.tile == 8 ? k_attn_q8_few<8> : (A.tile == 16 ? k_attn_q8_few<16> : k_attn_q8_few<32>);
-      static std::atomic<uint64_t> smem_few[3];
-      e = allow_smem(kernel, few_smem_bytes(A.tile), smem_few[A.tile == 8 ? 0 : (A.tile == 16 ? 1 : 2)]);
-      if (e == cudaSuccess) e = launch_dependent(kernel, dim3((unsigned)ctas), few_warps(A.tile) * 32, 1, few_smem_bytes(A.tile), st, true, P);
+      const auto launch = [&](auto kernel, std::atomic<uint64_t>& smem_set) {
+        const int smem = few_smem_bytes(A.tile, A.warps);
+        const cudaError_t set = allow_smem(kernel, smem, smem_set);
+        return set != cudaSuccess ? set : launch_dependent(kernel, dim3((unsigned)ctas), A.warps * 32, 1, smem, st, true, P);
+      };
+      static std::atomic<uint64_t> smem_few[8];
+      if (A.tile == 8) e = A.warps == 12 ? launch(k_attn_q8_few<8, 12>, smem_few[0]) : (A.warps == 6 ? launch(k_attn_q8_few<8, 6>, smem_few[1]) : launch(k_attn_q8_few<8, 4>, smem_few[2]));
+      else if (A.tile == 16) e = A.warps == 12 ? launch(k_attn_q8_few<16, 12>, smem_few[3]) : (A.warps == 6 ? launch(k_attn_q8_few<16, 6>, smem_few[4]) : launch(k_attn_q8_few<16, 4>, smem_few[5]));
+      else e = A.warps == 8 ? launch(k_attn_q8_few<32, 8>, smem_few[6]) : launch(k_attn_q8_few<32, 4>, smem_few[7]);
       *launches += 1;
     }
     if (e != cudaSuccess) { g_attn_last_error = (int)e; return OVGGT_ERR_CUDA; }
