@@ -100,6 +100,18 @@ def test_lengths_and_masks(seqs, M, heads, kv, capacity):
     _check(q, cache, lens, live)
 
 
+@pytest.mark.parametrize("seqs,M,heads,kv,capacity", [(300, 1, 2, 2, 96), (40, 1, 4, 4, 1536), (10, 1, 8, 8, 4096), (3, 1, 8, 8, 2048), (160, 3, 4, 2, 256), (300, 12, 1, 1, 96),
+                                                      (60, 12, 4, 4, 800), (5, 16, 16, 16, 2048), (2, 12, 4, 4, 2048), (300, 30, 1, 1, 96), (90, 20, 4, 4, 512), (7, 25, 16, 16, 1024)])
+def test_more_heads_than_multiprocessors(seqs, M, heads, kv, capacity):
+    """... and a half, and a third of them: an SM's warps in one CTA or in several, the cached rows in one part or in many."""
+    q, cache = _case(seqs, M, heads, kv, capacity, seed=3)
+    g = _g(seqs)
+    lens = torch.randint(0, capacity + 1, (seqs,), generator=g, device="cuda", dtype=torch.int32)
+    live = (torch.rand((seqs, capacity), generator=g, device="cuda") < 0.8).to(torch.uint8)
+    _check(q, cache, lens)
+    _check(q, cache, lens, live)
+
+
 @pytest.mark.parametrize("M", [1, 2, 40, 200, 700])
 def test_every_short_length(M):
     """Lengths 0 to 67 and around 192 at once: tiles that end anywhere, and none at all."""
