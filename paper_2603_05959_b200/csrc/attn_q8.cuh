@@ -657,7 +657,6 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
   unsigned char* sV = sK + kKVStages * kTileBytes;
   AttnBarriers* B = reinterpret_cast<AttnBarriers*>(smem + kManyBar);
   unsigned* top = reinterpret_cast<unsigned*>(B + 1);    // [8]
-  volatile int* range = reinterpret_cast<volatile int*>(top + 8);             // halves of this CTA, live rows from its first tile on: read where they are needed
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const Place at0(P, blockIdx.x);
   const int hk = at0.hk, part = at0.part, seq = at0.seq;
@@ -717,10 +716,6 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
     }
     most = __reduce_max_sync(0xFFFFFFFFu, most);
     if (lane == 0) top[warp] = most;
-    if (threadIdx.x == 0) {
-      range[0] = 2 * n_tiles;
-      range[1] = len - t_begin * kBN;
-    }
   }
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   tc_fence_before();
@@ -848,8 +843,9 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
       bound = sqrtf(qn2 * kmax2) * c;
       odd = !(zero == 0.0f);
     }
-    for (int idx = 0; idx < range[0] && ok; ++idx) {    // idx = 2 * tile + half
-      const int it = idx >> 1, hf = idx & 1, left = range[1] - idx * kHalf;
+    int idx = 0, left = min(len - t_begin * kBN, n_tiles * kBN);   // idx = 2 * tile + half; live rows from there on
+    for (; ok && ((idx & 1) != 0 || left > 0); ++idx, left -= kHalf) {
+      const int it = idx >> 1, hf = idx & 1;
       // (every wait result is made warp-uniform before the warp meets an .aligned tensor-memory instruction)
       ok = __all_sync(0xFFFFFFFFu, mbar_wait(&B->s_full[hf], (uint32_t)it & 1u, B, P.status)) != 0;
       if (!ok) break;
@@ -914,7 +910,7 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
         const bool grow = mx - m > kRescaleThreshold;
         if (__any_sync(0xFFFFFFFFu, grow)) {
           // O may still be accumulating the half before: the scores of the next half, issued behind it, tell; or the last one's own barrier
-          ok = idx + 1 < range[0] ? mbar_wait(&B->s_full[hf ^ 1], (uint32_t)((idx + 1) >> 1) & 1u, B, P.status)
+          ok = hf == 0 || left > kHalf ? mbar_wait(&B->s_full[hf ^ 1], (uint32_t)((idx + 1) >> 1) & 1u, B, P.status)
                                      : mbar_wait(&B->pv_done, 0, B, P.status);
           ok = __all_sync(0xFFFFFFFFu, ok) != 0;
           if (!ok) break;
@@ -944,7 +940,7 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
       tc_fence_before();
       mbar_arrive(&B->p_full[hf]);
     }
-    const bool seen = range[0] > 0;
+    const bool seen = idx > 0;
     if (seen && ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&B->o_full, 0, B, P.status)) != 0;
     if (ok) {
       tc_fence_after();
