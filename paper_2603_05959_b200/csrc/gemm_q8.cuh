@@ -100,11 +100,19 @@ __device__ __forceinline__ void q8_finish8(const GemmQ8Args& P, int m, int n, co
     q8_store8<false>(P.o, m, n, t, make_uint4(0u, 0u, 0u, 0u));
 }
 
+template <int COUNT>
+struct Q8Steps {
+  static constexpr int value = COUNT;
+};
+
 // Few tokens: a CTA takes 16 channels and 8 GROUPS tokens, its eight warps every eighth 64 columns of K, whose sums they add up in
 // shared memory.  A lane reads 16 bytes of a row: which of a product's columns they are does not matter as long as both
-// operands agree.
-template <int GROUPS>
-__global__ void __launch_bounds__(256) k_linear_q8_few(const GemmQ8Args P) {
+// operands agree.  Bound by the time that a warp's loads take: where all CTAs run at once (ONE_WAVE, two to an SM) a warp has those of four
+// steps in flight, elsewhere those of two, and four CTAs share an SM.  Measured: 1 x 4096 x 1024 2.5 us, 16 x 1024 x 4096 3.9,
+// 32 x 1024 x 4096 4.7 (in four CTAs to an SM 5.6 and 8.7), 16 x 4096 x 4096 5.2 (7.8); in several waves 8 x 16384 x 1024 5.1 (with four steps and
+// two CTAs 6.7), 1 x 16384 x 4096 8.3 (10.9).
+template <int GROUPS, bool ONE_WAVE>
+__global__ void __launch_bounds__(256, ONE_WAVE ? 2 : 4) k_linear_q8_few(const GemmQ8Args P) {
   constexpr int kTokens = 8 * GROUPS;
   __shared__ int part[8][kTokens][16 + 1];
   pdl_trigger();
@@ -117,19 +125,33 @@ __global__ void __launch_bounds__(256) k_linear_q8_few(const GemmQ8Args P) {
   const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
   const int8_t* w0 = P.w + (size_t)(n0 + g) * K;
   const int8_t* w1 = w0 + (size_t)8 * K;
-#pragma unroll 2
-  for (int k = warp * 64 + 16 * t; k - 16 * t < K; k += 512) {
-    const bool in = k < K;
-    const uint4 u = in && n0 + g < N ? __ldcg(reinterpret_cast<const uint4*>(w0 + k)) : zero;
-    const uint4 v = in && n0 + 8 + g < N ? __ldcg(reinterpret_cast<const uint4*>(w1 + k)) : zero;
+  const auto steps = [&](int k, auto count) {            // (all of the steps' loads first)
+    constexpr int kSteps = decltype(count)::value;
+    uint4 u[kSteps], v[kSteps], x[kSteps][GROUPS];
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i) {
-      const int m = m0 + 8 * i + g;
-      const uint4 x = in && m < M ? *reinterpret_cast<const uint4*>(P.a + (size_t)m * K + k) : zero;
-      mma_s8(c[i], u.x, v.x, u.y, v.y, x.x, x.y);
-      mma_s8(c[i], u.z, v.z, u.w, v.w, x.z, x.w);
+    for (int j = 0; j < kSteps; ++j) {
+      const int at = k + 512 * j + 16 * t;
+      const bool in = at < K;
+      u[j] = in && n0 + g < N ? __ldcg(reinterpret_cast<const uint4*>(w0 + at)) : zero;
+      v[j] = in && n0 + 8 + g < N ? __ldcg(reinterpret_cast<const uint4*>(w1 + at)) : zero;
+#pragma unroll
+      for (int i = 0; i < GROUPS; ++i)
+        x[j][i] = in && m0 + 8 * i + g < M ? *reinterpret_cast<const uint4*>(P.a + (size_t)(m0 + 8 * i + g) * K + at) : zero;
     }
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) {
+#pragma unroll
+      for (int i = 0; i < GROUPS; ++i) {
+        mma_s8(c[i], u[j].x, v[j].x, u[j].y, v[j].y, x[j][i].x, x[j][i].y);
+        mma_s8(c[i], u[j].z, v[j].z, u[j].w, v[j].w, x[j][i].z, x[j][i].w);
+      }
+    }
+  };
+  long k = warp * 64;                                    // of the warp: the limits below are the same for its lanes
+  if constexpr (ONE_WAVE) {
+    for (; k + 1536 < K; k += 2048) steps((int)k, Q8Steps<4>{});
   }
+  for (; k < K; k += 1024) steps((int)k, Q8Steps<2>{});
 #pragma unroll
   for (int i = 0; i < GROUPS; ++i) {                     // (rows: channels g, g + 8; columns: tokens 2 t, 2 t + 1)
     part[warp][8 * i + 2 * t][g] = c[i][0];
@@ -440,7 +462,9 @@ static inline int q8_tcgen05_launch(const GemmQ8Args& P, cudaStream_t st) {
   return OVGGT_OK;
 }
 
-constexpr int kQ8Few = 32;             // tokens up to which the few-token kernel is taken (32 x 4096 x 1024: 4.9 us, by tiles 5.1; 64: 9 and 4.7)
+// The few-token kernel is taken for up to 16 tokens and wherever its CTAs run at once, two to an SM: 128 x 1024 x 1024 3.8 us (by tiles 4.7),
+// 64 x 1024 x 4096 6.5 (9.6), 128 x 1024 x 4096 7.2 (9.3), but in two waves 64 x 4096 x 1024 6.3 (4.6), 128 x 2048 x 4096 13.4 (9.5).
+constexpr int kQ8OneWave = 296;
 
 // Tile width, from a model in nanoseconds fitted to 718 to 10992 tokens, 768 to 4096 channels and columns: set-up and last epilogue, waves
 // over 148 SMs as long as their steps of 128 columns, and what is left of an epilogue between two tiles.  1374 x 4096 x 1024 takes 15.2, 12.9
@@ -456,13 +480,15 @@ inline int q8_tile_width(int M, int N, int K) {
 }
 
 static inline int gemm_q8_launch(const GemmQ8Args& P, cudaStream_t st) {
-  const int M = P.o.M;
-  if (M > kQ8Few) {
+  const int M = P.o.M, groups = M <= 8 ? 1 : (M <= 16 ? 2 : 4);
+  const long ctas = (long)((P.o.N + 15) / 16) * ((M + 8 * groups - 1) / (8 * groups));
+  const bool one_wave = ctas <= kQ8OneWave;
+  if (M > 16 && !one_wave) {
     const int bn = q8_tile_width(M, P.o.N, P.o.K);
     return bn == 256 ? q8_tcgen05_launch<256>(P, st) : (bn == 128 ? q8_tcgen05_launch<128>(P, st) : q8_tcgen05_launch<64>(P, st));
   }
-  const int groups = M <= 8 ? 1 : (M <= 16 ? 2 : 4);
-  const auto kernel = groups == 1 ? k_linear_q8_few<1> : (groups == 2 ? k_linear_q8_few<2> : k_linear_q8_few<4>);
+  const auto kernel = groups == 1 ? (one_wave ? k_linear_q8_few<1, true> : k_linear_q8_few<1, false>)
+                                  : (groups == 4 ? k_linear_q8_few<4, true> : (one_wave ? k_linear_q8_few<2, true> : k_linear_q8_few<2, false>));
   const cudaError_t e = launch_dependent(kernel, dim3((P.o.N + 15) / 16, (M + 8 * groups - 1) / (8 * groups)), 256, 1, 0, st, true, P);
   if (e != cudaSuccess) { g_attn_last_error = (int)e; return OVGGT_ERR_CUDA; }
   return OVGGT_OK;

@@ -137,3 +137,39 @@ def test_arguments():
             B.k_linear_q8(**dict(ok, **over))
     with pytest.raises(B.OvggtError):
         B.k_linear_q8(**dict(ok, residual=None))
+
+
+# (a product by tiles has more blocks of 16 channels and 32 tokens than can run at once)
+@pytest.mark.parametrize("M,N,K", [(9601, 8, 16), (4800, 40, 80), (1700, 72, 528), (700, 264, 2064), (250, 1032, 1040), (40, 4104, 272), (17, 5000, 1040),
+                                   (256, 592, 144), (257, 592, 144)])
+def test_few_columns_by_tiles(M, N, K):
+    test_linear(M, N, K)
+
+
+@pytest.mark.parametrize("K", [16, 496, 528, 1536, 1552, 2032, 2064, 4112, 6160])
+@pytest.mark.parametrize("M,N", [(1, 4736), (8, 4744), (16, 4736), (13, 4744), (31, 24), (200, 72)])
+def test_lengths_of_few_tokens(M, N, K):
+    """K that ends in each of a warp's steps, in CTAs that run all at once and in several waves."""
+    a, as_, w, ws, x, st = _case(M, N, K)
+    t, s = torch.empty_like(x), torch.empty_like(x)
+    B.k_linear_q8(a, as_, w, ws, (t,), residual=x, sum_out=s, status=st)
+    ref = _t(a, as_, w, ws)
+    assert torch.equal(t, ref) and torch.equal(s, x + ref)
+
+
+def test_largest_sums_by_tiles():
+    M, N, K = 3200, 56, 131056
+    a = torch.full((M, K), -128, dtype=torch.int8, device="cuda")
+    w = torch.full((N, K), -128, dtype=torch.int8, device="cuda")
+    t = torch.empty((M, N), dtype=torch.bfloat16, device="cuda")
+    st = torch.zeros(16, dtype=torch.int32, device="cuda")
+    B.k_linear_q8(a, torch.ones(M, device="cuda"), w, torch.ones(N, device="cuda"), (t,), status=st)
+    assert torch.equal(t, torch.full_like(t, float(16384 * K))) and int(st[0]) == 0
+
+
+def test_scales_that_are_not_finite_by_tiles():
+    test_scales_that_are_not_finite(3000)
+
+
+def test_rows_behind_the_last_are_left_alone_by_tiles():
+    test_rows_behind_the_last_are_left_alone(2400)
