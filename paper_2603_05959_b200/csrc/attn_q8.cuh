@@ -28,6 +28,12 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// The first product of a sum that begins at `on`.
+__device__ __forceinline__ void mma_s8_on(int (&c)[4], uint32_t on, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+               : "=r"(c[0]), "=r"(c[1]), "=r"(c[2]), "=r"(c[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "r"(on));
+}
 __device__ __forceinline__ void mma_u8s8(int (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3])
@@ -49,6 +55,10 @@ __device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b) {
   const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
   return *reinterpret_cast<const uint32_t*>(&d);
 }
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  const __nv_bfloat162 d = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&d);
+}
 // Two int8, the low bytes of the halves of x, as a pair of bf16, exact: 128 + the low seven bits, less 128 or, of a negative one, 256.
 __device__ __forceinline__ uint32_t int8_to_bf16x2(uint32_t x) { return sub_bf16x2((x & 0x007F007Fu) | 0x43004300u, (x & 0x00800080u) | 0x43004300u); }
 
@@ -58,13 +68,14 @@ __device__ __forceinline__ uint32_t int8_to_bf16x2(uint32_t x) { return sub_bf16
 // copy, MMA, exponentials and MMA that a dozen warps an SM do not cover.  A warp takes tiles of 32 cached rows by itself, with three of them on their way in its own stages
 // (no barrier in the loop); the warps' results are joined through shared memory, those of the CTAs that share a sequence and head (parts) by
 // the bf16 attention's merge kernel.
-//   scores  by int8 MMAs on the cached bytes as they are.  A row of Q is taken as whole numbers of 15 bits, q = 2^(e - 13) (256 hi + lo), two int8
-//           operands: exact for elements down to 2^-6 of the row's largest, to 2^-14 of it for the rest.  With at
-//           most 8 rows hi and lo are the two halves of one operand of 16 rows.
+//   scores  from queries that keep every bit.  With at most 8 rows by int8 MMAs on the cached bytes as they are: a row of Q is taken as whole
+//           numbers of 31 bits in units of 2^-29 of its largest power of two, four int8 operands in the halves of two; where that would not
+//           be exact (a row with elements below 2^-22 of its largest), and with more rows, by bf16 MMAs on Q itself and the cached bytes
+//           made bf16.  (One row over 32768, 16 heads: 19.5 us, by bf16 MMAs 22.0; two operands' 15 bits took 18.4 and lost a row's small elements.)
 //   P V     with at most 8 rows by int8 MMAs too: a weight p 2^(x - 133) as a whole number of 31 bits, 2^-28 of a reference that follows the largest
 //           weight, four unsigned bytes in the halves of two operands; the cached bytes of four rows are only put side by side.  The int32 sums
 //           are exact and go into fp32 when the reference moves.  With more rows, where that many sums do not fit the registers, by bf16 MMAs: the
-//           cached bytes are exact in bf16, a weight is rounded to it (2^-8).  (One row over 32768, 16 heads: 18 us, by bf16 MMAs 22.)
+//           cached bytes are exact in bf16, a weight is rounded to it (2^-8).
 // Which cached row or column an operand's row or column stands for is free, so each lane takes 16 bytes of a K row and 8
 // bytes of a V row at once.
 // An SM holds as many warps as their registers leave without spilling (four tokens over up to 16384 rows by 16 warps 28 us, by 12 25; 16 rows
@@ -74,9 +85,7 @@ constexpr int kFewStages = 3, kFewKeys = 32;
 constexpr int kFewX = 2 * kFewKeys * 64;                 // of a stage: K, V, then the exponents of K and V and the mask, 32 bytes each
 constexpr int kFewStage = kFewX + 128;
 constexpr int kFewTable = kFewKeys * 16;                 // of a warp: (step of K, 0 or -inf under the mask, step of V) for each row of its tile
-__host__ __device__ constexpr int few_smem_bytes(int rows, int warps) {
-  return warps * (kFewStages * kFewStage + kFewTable) + (rows == 8 ? 1 : rows / 8) * 1024 + rows * 8;
-}
+__host__ __device__ constexpr int few_smem_bytes(int warps) { return warps * (kFewStages * kFewStage + kFewTable); }
 static_assert(kFewStages * kFewStage >= 32 * (64 + 2) * 4, "a warp's result does not fit its stages");
 
 template <int ROWS, int kFewWarps>
@@ -138,67 +147,79 @@ __global__ void __launch_bounds__(kFewWarps * 32, few_warps(ROWS) / kFewWarps) k
 #pragma unroll
   for (int s = 0; s < kFewStages - 1; ++s) request(first + s * stride, s);
 
-  // ---- the operands of Q, eight rows a warp, by way of shared memory: [tile][0: hi (or hi and lo), 1: lo][32 columns][register]
-  constexpr int L = PACK ? 1 : 2;
-  uint4* q_sh = reinterpret_cast<uint4*>(smem + kFewWarps * (kFewStages * kFewStage + kFewTable));      // [T][L][2][lane]
-  float2* f_sh = reinterpret_cast<float2*>(q_sh + T * L * 2 * 32);                                        // [ROWS]
-  if (warp < T * R) {
-    const int i = warp / R, half = warp % R, r = row0 + 16 * i + 8 * half + g;
-    float x[16];
-#pragma unroll
-    for (int e = 0; e < 16; ++e) x[e] = 0.0f;
-    if (r < rows) {
-      const uint4* p = reinterpret_cast<const uint4*>(P.q + q_at(r) + 16 * t);
-      unpack<kBF16>(p[0], x);
-      unpack<kBF16>(p[1], x + 8);
-    }
-    uint32_t most = 0;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) most = max(most, __float_as_uint(x[e]) & 0x7FFFFFFFu);
-    most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
-    most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
-    const int e2 = (int)(most >> 23) - 127, up = 13 - e2;
-    const bool finite = most < 0x7F800000u, some = finite && most >= 0x00800000u;
-    const float u0 = some ? __int_as_float((up / 2 + 127) << 23) : 0.0f, u1 = some ? __int_as_float((up - up / 2 + 127) << 23) : 0.0f;
-    // log2(e) / 8 2^(e - 13) 2^-6: cached values are 2^(x - 133)
-    if (t == 0) f_sh[16 * i + 8 * half + g] = make_float2(some ? ldexpf(1.4426950408889634f * 0.125f, e2 - 19) : 0.0f, finite ? 0.0f : 1.0f);
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      int hi[4], lo[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int z = some ? __float2int_rn(x[4 * w + e] * u0 * u1) : 0;
-        hi[e] = (z + 128) >> 8;
-        lo[e] = z - hi[e] * 256;
-      }
-      const uint32_t ph = (hi[0] & 255) | (hi[1] & 255) << 8 | (hi[2] & 255) << 16 | (uint32_t)hi[3] << 24;
-      const uint32_t pl = (lo[0] & 255) | (lo[1] & 255) << 8 | (lo[2] & 255) << 16 | (uint32_t)lo[3] << 24;
-      // word w: columns 16 t + 4 w on: k-step w / 2, its first or second half; register of the operand: + 1 for rows 8 to 15
-      uint32_t* at = reinterpret_cast<uint32_t*>(q_sh + ((i * L) * 2 + (w >> 1)) * 32 + lane) + (w & 1) * 2;
-      if constexpr (PACK) {
-        at[0] = ph;
-        at[1] = pl;
-      } else {
-        at[half] = ph;
-        at[2 * 32 * 4 + half] = pl;
-      }
-    }
-  }
-  __syncthreads();
-  uint32_t qa[T][L][2][4];
-  float f[T][R];                                         // a score in log2 units is f x the whole numbers' product x 2^(kx - 127)
+  // ---- the operands of Q: of a row the 16 columns of which this lane reads K, two by two as K's bytes come apart, times the power of two
+  // that brings the row's largest near one (a query may have any size, and the products' sums are fp32)
+  // [four of its columns]: row g, (row g + 8,) columns 0 and 2 of them, then 1 and 3; or the four bytes of all four columns, from the highest
+  uint32_t qa[T][4][PACK ? 4 : 2 * R];
+  float f[T][R];                                         // a score in log2 units is f x the product with the whole numbers x 2^(kx - 127)
   bool odd[T][R];                                        // a query that is not finite: its result is not a number
+  bool wide = false;                                     // of this warp's rows: some element is below 2^-22 of its row's largest
 #pragma unroll
-  for (int i = 0; i < T; ++i) {
-#pragma unroll
-    for (int p = 0; p < 2 * L; ++p) *reinterpret_cast<uint4*>(qa[i][p >> 1][p & 1]) = q_sh[(i * 2 * L + p) * 32 + lane];
+  for (int i = 0; i < T; ++i)
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const float2 x = f_sh[16 * i + 8 * r + g];
-      f[i][r] = x.x;
-      odd[i][r] = x.y != 0.0f;
+      const int row = row0 + 16 * i + 8 * r + g;
+      uint4 x[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
+      if (row < rows) {
+        const uint4* p = reinterpret_cast<const uint4*>(P.q + q_at(row) + 16 * t);
+        x[0] = p[0];
+        x[1] = p[1];
+      }
+      uint32_t* w = &x[0].x;
+      uint32_t most = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) most = max(most, max(w[e] << 16 & 0x7FFFFFFFu, w[e] & 0x7FFF0000u));
+      most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
+      most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
+      odd[i][r] = most >= 0x7F800000u;
+      const int e2 = min(max((int)(most >> 23) - 127, -100), 126);            // (down to 2^-100 and no further: f stays normal)
+      const uint32_t scale = odd[i][r] ? 0u : (uint32_t)(127 - e2) << 7 | (uint32_t)(127 - e2) << 23;
+      f[i][r] = 1.4426950408889634f * 0.125f * __int_as_float((e2 - 6 + 127) << 23);       // (2^-6: cached values are 2^(x - 133))
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = odd[i][r] ? 0u : mul_bf16x2(w[j], scale);
+      if constexpr (PACK) {
+        // (now in units of 2^-29: whole numbers of 31 bits as long as no element is below 2^-22)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const uint32_t a = w[j] << 16 & 0x7FFFFFFFu, b = w[j] & 0x7FFF0000u;
+          wide |= (a != 0u && a < 0x34800000u) || (b != 0u && b < 0x34800000u);
+        }
+        wide = __any_sync(0xFFFFFFFFu, wide) != 0;
+        if (wide) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            qa[0][j][0] = __byte_perm(w[2 * j], w[2 * j + 1], 0x5410);
+            qa[0][j][1] = __byte_perm(w[2 * j], w[2 * j + 1], 0x7632);
+            qa[0][j][2] = qa[0][j][3] = 0u;
+          }
+        } else {
+          f[0][0] *= 0.03125f;                           // (the highest byte counts 2^24 units)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {                  // four columns: their bytes, from the highest, each rounded so that what is left fits a signed byte
+            uint32_t plane[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t half = w[2 * j + (e >> 1)];
+              int z = __float2int_rn(__uint_as_float(e & 1 ? half & 0xFFFF0000u : half << 16) * 536870912.0f);
+#pragma unroll
+              for (int b = 3; b >= 0; --b) {
+                const int low = (int)(int8_t)z;
+                plane[b] |= ((uint32_t)low & 255u) << 8 * e;
+                z = (z - low) >> 8;
+              }
+            }
+#pragma unroll
+            for (int b = 0; b < 4; ++b) qa[0][j][b] = plane[b];
+          }
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          qa[i][j][r] = __byte_perm(w[2 * j], w[2 * j + 1], 0x5410);
+          qa[i][j][R + r] = __byte_perm(w[2 * j], w[2 * j + 1], 0x7632);
+        }
+      }
     }
-  }
 
   float m[T][R], l[T][R], o[T][8][4];                    // O: with at most 8 rows two columns a register pair, [0] and [1]
   int c1[PACK ? 8 : 1][4], c2[PACK ? 8 : 1][4], since = 0;   // what the int8 MMAs have summed up since O was last brought up to date, in how many tiles
@@ -228,181 +249,205 @@ __global__ void __launch_bounds__(kFewWarps * 32, few_warps(ROWS) / kFewWarps) k
 #pragma unroll
     for (int d = 0; d < 8; ++d) o[i][d][0] = o[i][d][1] = o[i][d][2] = o[i][d][3] = 0.0f;
   }
-  int stage = 0;
+  auto stream = [&](auto by_bytes) {                     // the loop over this warp's tiles
+    constexpr bool kBytes = decltype(by_bytes)::value;     // Q by its bytes
+    int stage = 0;
 #pragma unroll 1
-  for (int tile = first; tile < tiles; tile += stride) {
-    asm volatile("cp.async.wait_group %0;" ::"n"(kFewStages - 2) : "memory");
-    __syncwarp();                                        // this tile has arrived, and all lanes are done with the one before
-    request(tile + (kFewStages - 1) * stride, stage == 0 ? kFewStages - 1 : stage - 1);
-    const unsigned char* s = stages + stage * kFewStage;
-    stage = stage + 1 == kFewStages ? 0 : stage + 1;
+    for (int tile = first; tile < tiles; tile += stride) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kFewStages - 2) : "memory");
+      __syncwarp();                                        // this tile has arrived, and all lanes are done with the one before
+      request(tile + (kFewStages - 1) * stride, stage == 0 ? kFewStages - 1 : stage - 1);
+      const unsigned char* s = stages + stage * kFewStage;
+      stage = stage + 1 == kFewStages ? 0 : stage + 1;
 
-    {                                                    // a lane a row: what its scores and its weight are multiplied with
-      const bool in = tile * kFewKeys + lane < len && (P.live == nullptr || s[kFewX + 64 + lane] != 0);
-      // (255: infinity, which a block of zeros makes NaN)
-      const uint32_t vx = s[kFewX + 32 + lane];
-      const float ks = __int_as_float((int)s[kFewX + lane] << 23);
-      if constexpr (PACK)                                // (the exponent of the value's step; a value that is not finite takes its score with it)
-        table[lane] = in ? make_float4(ks, vx == 255u ? __int_as_float(0x7FC00000) : 0.0f, (float)((int)vx - 133), 0.0f) : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
-      else
-        table[lane] = in ? make_float4(ks, 0.0f, q8_step(vx), 0.0f) : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
-    }
-    __syncwarp();
-    float sc[T][R][8], vs[8];                            // scores of keys 8 b + t (even entries) and 8 b + t + 4
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const uint4 kw = *reinterpret_cast<const uint4*>(s + (8 * b + g) * 64 + t * 16);
-      float4 x[2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        x[e] = table[8 * b + t + 4 * e];
-        vs[2 * b + e] = x[e].z;
+      {                                                    // a lane a row: what its scores and its weight are multiplied with
+        const bool in = tile * kFewKeys + lane < len && (P.live == nullptr || s[kFewX + 64 + lane] != 0);
+        // (255: infinity, which a block of zeros makes NaN)
+        const uint32_t vx = s[kFewX + 32 + lane];
+        const float ks = __int_as_float((int)s[kFewX + lane] << 23);
+        if constexpr (PACK)                                // (the exponent of the value's step; a value that is not finite takes its score with it)
+          table[lane] = in ? make_float4(ks, vx == 255u ? __int_as_float(0x7FC00000) : 0.0f, (float)((int)vx - 133), 0.0f) : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
+        else
+          table[lane] = in ? make_float4(ks, 0.0f, q8_step(vx), 0.0f) : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
       }
+      __syncwarp();
+      float sc[T][R][8], vs[8];                            // scores of keys 8 b + t (even entries) and 8 b + t + 4
 #pragma unroll
-      for (int i = 0; i < T; ++i) {
-        int c[4];
-        mma_s8_first(c, qa[i][0][0][0], qa[i][0][0][1], qa[i][0][0][2], qa[i][0][0][3], kw.x, kw.y);
-        mma_s8(c, qa[i][0][1][0], qa[i][0][1][1], qa[i][0][1][2], qa[i][0][1][3], kw.z, kw.w);
-        if constexpr (PACK) {
+      for (int b = 0; b < 4; ++b) {
+        const uint4 kw = *reinterpret_cast<const uint4*>(s + (8 * b + g) * 64 + t * 16);
+        float4 x[2];
 #pragma unroll
-          for (int e = 0; e < 2; ++e) sc[i][0][2 * b + e] = fmaf((float)(c[e] * 256 + c[e + 2]), f[i][0] * x[e].x, x[e].y);
+        for (int e = 0; e < 2; ++e) {
+          x[e] = table[8 * b + t + 4 * e];
+          vs[2 * b + e] = x[e].z;
+        }
+        if constexpr (kBytes) {
+          // (sums of at most 2^20 in size, on top of 1.5 2^23: read as fp32 they need no conversion)
+          constexpr uint32_t kMagic = 0x4B400000u;
+          int c[4], d[4];
+          mma_s8_on(c, kMagic, qa[0][0][0], qa[0][0][1], qa[0][1][0], qa[0][1][1], kw.x, kw.y);
+          mma_s8(c, qa[0][2][0], qa[0][2][1], qa[0][3][0], qa[0][3][1], kw.z, kw.w);
+          mma_s8_on(d, kMagic, qa[0][0][2], qa[0][0][3], qa[0][1][2], qa[0][1][3], kw.x, kw.y);
+          mma_s8(d, qa[0][2][2], qa[0][2][3], qa[0][3][2], qa[0][3][3], kw.z, kw.w);
+          const float2 back = make_float2(-12582912.0f, -12582912.0f), down = make_float2(0.00390625f, 0.00390625f);
+          float2 y = add2(make_float2(__int_as_float(d[2]), __int_as_float(d[3])), back);
+          y = fma2(y, down, add2(make_float2(__int_as_float(d[0]), __int_as_float(d[1])), back));
+          y = fma2(y, down, add2(make_float2(__int_as_float(c[2]), __int_as_float(c[3])), back));
+          y = fma2(y, down, add2(make_float2(__int_as_float(c[0]), __int_as_float(c[1])), back));
+          sc[0][0][2 * b] = fmaf(y.x, f[0][0] * x[0].x, x[0].y);
+          sc[0][0][2 * b + 1] = fmaf(y.y, f[0][0] * x[1].x, x[1].y);
         } else {
-          int d[4];
-          mma_s8_first(d, qa[i][1][0][0], qa[i][1][0][1], qa[i][1][0][2], qa[i][1][0][3], kw.x, kw.y);
-          mma_s8(d, qa[i][1][1][0], qa[i][1][1][1], qa[i][1][1][2], qa[i][1][1][3], kw.z, kw.w);
+          float c[T][4];
 #pragma unroll
-          for (int r = 0; r < R; ++r)
+          for (int i = 0; i < T; ++i) c[i][0] = c[i][1] = c[i][2] = c[i][3] = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) sc[i][r][2 * b + e] = fmaf((float)(c[2 * r + e] * 256 + d[2 * r + e]), f[i][r] * x[e].x, x[e].y);
+          for (int j = 0; j < 4; ++j) {                    // four bytes of a key: columns 0 and 2, 1 and 3
+            const uint32_t four = j == 0 ? kw.x : (j == 1 ? kw.y : (j == 2 ? kw.z : kw.w));
+            const uint32_t b0 = int8_to_bf16x2(four), b1 = int8_to_bf16x2(four >> 8);
+#pragma unroll
+            for (int i = 0; i < T; ++i) mma_bf16(c[i], qa[i][j][0], PACK ? 0u : qa[i][j][1], qa[i][j][R], PACK ? 0u : qa[i][j][2 * R - 1], b0, b1);
+          }
+#pragma unroll
+          for (int i = 0; i < T; ++i)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) sc[i][r][2 * b + e] = fmaf(c[i][2 * r + e], f[i][r] * x[e].x, x[e].y);
         }
       }
-    }
-    // the running maximum moves only when it is outgrown by 2^8
-    float top[T][R];
-    bool grown = false;
-#pragma unroll
-    for (int i = 0; i < T; ++i)
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        float x = sc[i][r][0];
-#pragma unroll
-        for (int e = 1; e < 8; ++e) x = fmaxf(x, sc[i][r][e]);
-        x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 1));
-        top[i][r] = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 2));
-        grown |= top[i][r] > m[i][r] + kRescaleThreshold;
-      }
-    float topv = -INFINITY;
-    if constexpr (PACK) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) topv = fmaxf(topv, sc[0][0][e] + vs[e]);
-      topv = fmaxf(topv, __shfl_xor_sync(0xFFFFFFFFu, topv, 1));
-      topv = fmaxf(topv, __shfl_xor_sync(0xFFFFFFFFu, topv, 2));
-      grown |= topv > mv + kRoom || since >= kSumsMost;
-    }
-    if (__any_sync(0xFFFFFFFFu, grown)) {
-      if constexpr (PACK) {
-        const float mn = fmaxf(mv, topv);
-        if (since > 0) take_sums(mv == mn ? 1.0f : ex2(mv - mn));
-        mv = mn;
-      }
+      // the running maximum moves only when it is outgrown by 2^8
+      float top[T][R];
+      bool grown = false;
 #pragma unroll
       for (int i = 0; i < T; ++i)
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-          const float mn = fmaxf(m[i][r], top[i][r]), corr = m[i][r] == mn ? 1.0f : ex2(m[i][r] - mn);
-          m[i][r] = mn;
-          l[i][r] *= corr;
-          if constexpr (!PACK) {
+          float x = sc[i][r][0];
 #pragma unroll
-            for (int d = 0; d < 8; ++d) {
-              o[i][d][2 * r] *= corr;
-              o[i][d][2 * r + 1] *= corr;
+          for (int e = 1; e < 8; ++e) x = fmaxf(x, sc[i][r][e]);
+          x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 1));
+          top[i][r] = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 2));
+          grown |= top[i][r] > m[i][r] + kRescaleThreshold;
+        }
+      float topv = -INFINITY;
+      if constexpr (PACK) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) topv = fmaxf(topv, sc[0][0][e] + vs[e]);
+        topv = fmaxf(topv, __shfl_xor_sync(0xFFFFFFFFu, topv, 1));
+        topv = fmaxf(topv, __shfl_xor_sync(0xFFFFFFFFu, topv, 2));
+        grown |= topv > mv + kRoom || since >= kSumsMost;
+      }
+      if (__any_sync(0xFFFFFFFFu, grown)) {
+        if constexpr (PACK) {
+          const float mn = fmaxf(mv, topv);
+          if (since > 0) take_sums(mv == mn ? 1.0f : ex2(mv - mn));
+          mv = mn;
+        }
+#pragma unroll
+        for (int i = 0; i < T; ++i)
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            const float mn = fmaxf(m[i][r], top[i][r]), corr = m[i][r] == mn ? 1.0f : ex2(m[i][r] - mn);
+            m[i][r] = mn;
+            l[i][r] *= corr;
+            if constexpr (!PACK) {
+#pragma unroll
+              for (int d = 0; d < 8; ++d) {
+                o[i][d][2 * r] *= corr;
+                o[i][d][2 * r + 1] *= corr;
+              }
+            }
+          }
+      }
+      if constexpr (PACK) {
+        const float ref = m[0][0] == -INFINITY ? 0.0f : m[0][0], refv = mv == -INFINITY ? 0.0f : mv - kUnits;
+        const float2 back = make_float2(-ref, -ref), backv = make_float2(-refv, -refv);
+        float2 sum = make_float2(0.0f, 0.0f);
+        uint32_t w[8];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const float2 x = make_float2(sc[0][0][2 * b], sc[0][0][2 * b + 1]), d = add2(x, back), y = add2(add2(x, make_float2(vs[2 * b], vs[2 * b + 1])), backv);
+          sum = add2(sum, make_float2(ex2(d.x), ex2(d.y)));
+          w[2 * b] = __float2uint_rn(ex2(y.x));
+          w[2 * b + 1] = __float2uint_rn(ex2(y.y));
+        }
+        l[0][0] += sum.x + sum.y;
+        // operands: row g the top byte of the weights (a1) or the second lowest (a2), row g + 8 the byte below; 4 k's a register
+        uint32_t a1[4], a2[4], x[4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          transpose4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3], x);
+          a1[2 * h] = x[3];
+          a1[2 * h + 1] = x[2];
+          a2[2 * h] = x[1];
+          a2[2 * h + 1] = x[0];
+        }
+        uint2 v[8];                                        // rows t, t + 4, ...: the order of the weights
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = *reinterpret_cast<const uint2*>(s + 2048 + (t + 4 * e) * 64 + (((g >> 1) ^ (t & 2)) * 16) + (g & 1) * 8);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {             // four columns
+          uint32_t b0[4], b1[4];
+          transpose4(half ? v[0].y : v[0].x, half ? v[1].y : v[1].x, half ? v[2].y : v[2].x, half ? v[3].y : v[3].x, b0);
+          transpose4(half ? v[4].y : v[4].x, half ? v[5].y : v[5].x, half ? v[6].y : v[6].x, half ? v[7].y : v[7].x, b1);
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            mma_u8s8(c1[4 * half + d], a1, b0[d], b1[d]);
+            mma_u8s8(c2[4 * half + d], a2, b0[d], b1[d]);
+          }
+        }
+        ++since;                                           // (the same in every lane)
+      } else {
+        uint32_t pa[T][2][4];                                // P of 16 keys as an operand
+#pragma unroll
+        for (int i = 0; i < T; ++i)
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            const float ref = m[i][r] == -INFINITY ? 0.0f : m[i][r];
+            const float2 back = make_float2(-ref, -ref);
+            float2 sum = make_float2(0.0f, 0.0f);
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+              const float2 d = add2(make_float2(sc[i][r][2 * b], sc[i][r][2 * b + 1]), back), p = make_float2(ex2(d.x), ex2(d.y));
+              sum = add2(sum, p);
+              const float w0 = p.x * vs[2 * b], w1 = p.y * vs[2 * b + 1];
+              pa[i][b >> 1][(b & 1) * 2 + r] = pack_bf16(w0, w1);
+            }
+            l[i][r] += sum.x + sum.y;
+          }
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {                        // 16 keys: 16 b + t, + 4, + 8, + 12
+          uint2 v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int key = 16 * b + t + 4 * e;
+            v[e] = *reinterpret_cast<const uint2*>(s + 2048 + key * 64 + (((g >> 1) ^ (t & 2)) * 16) + (g & 1) * 8);
+          }
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {             // four columns: pairs of keys side by side, then one column of both a register
+            uint32_t w[2][2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const uint32_t x = half ? v[2 * e].y : v[2 * e].x, y = half ? v[2 * e + 1].y : v[2 * e + 1].x;
+              w[e][0] = __byte_perm(x, y, 0x5410);           // columns 0 and 1 of both, then 2 and 3
+              w[e][1] = __byte_perm(x, y, 0x7632);
+            }
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+              const uint32_t b0 = int8_to_bf16x2(w[0][d >> 1] >> (d & 1) * 8), b1 = int8_to_bf16x2(w[1][d >> 1] >> (d & 1) * 8);
+#pragma unroll
+              for (int i = 0; i < T; ++i) mma_bf16(o[i][4 * half + d], pa[i][b][0], pa[i][b][1], pa[i][b][2], pa[i][b][3], b0, b1);
             }
           }
         }
-    }
-    if constexpr (PACK) {
-      const float ref = m[0][0] == -INFINITY ? 0.0f : m[0][0], refv = mv == -INFINITY ? 0.0f : mv - kUnits;
-      const float2 back = make_float2(-ref, -ref), backv = make_float2(-refv, -refv);
-      float2 sum = make_float2(0.0f, 0.0f);
-      uint32_t w[8];
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const float2 x = make_float2(sc[0][0][2 * b], sc[0][0][2 * b + 1]), d = add2(x, back), y = add2(add2(x, make_float2(vs[2 * b], vs[2 * b + 1])), backv);
-        sum = add2(sum, make_float2(ex2(d.x), ex2(d.y)));
-        w[2 * b] = __float2uint_rn(ex2(y.x));
-        w[2 * b + 1] = __float2uint_rn(ex2(y.y));
-      }
-      l[0][0] += sum.x + sum.y;
-      // operands: row g the top byte of the weights (a1) or the second lowest (a2), row g + 8 the byte below; 4 k's a register
-      uint32_t a1[4], a2[4], x[4];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        transpose4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3], x);
-        a1[2 * h] = x[3];
-        a1[2 * h + 1] = x[2];
-        a2[2 * h] = x[1];
-        a2[2 * h + 1] = x[0];
-      }
-      uint2 v[8];                                        // rows t, t + 4, ...: the order of the weights
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = *reinterpret_cast<const uint2*>(s + 2048 + (t + 4 * e) * 64 + (((g >> 1) ^ (t & 2)) * 16) + (g & 1) * 8);
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {             // four columns
-        uint32_t b0[4], b1[4];
-        transpose4(half ? v[0].y : v[0].x, half ? v[1].y : v[1].x, half ? v[2].y : v[2].x, half ? v[3].y : v[3].x, b0);
-        transpose4(half ? v[4].y : v[4].x, half ? v[5].y : v[5].x, half ? v[6].y : v[6].x, half ? v[7].y : v[7].x, b1);
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          mma_u8s8(c1[4 * half + d], a1, b0[d], b1[d]);
-          mma_u8s8(c2[4 * half + d], a2, b0[d], b1[d]);
-        }
-      }
-      ++since;                                           // (the same in every lane)
-    } else {
-      uint32_t pa[T][2][4];                                // P of 16 keys as an operand
-#pragma unroll
-      for (int i = 0; i < T; ++i)
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-          const float ref = m[i][r] == -INFINITY ? 0.0f : m[i][r];
-          const float2 back = make_float2(-ref, -ref);
-          float2 sum = make_float2(0.0f, 0.0f);
-#pragma unroll
-          for (int b = 0; b < 4; ++b) {
-            const float2 d = add2(make_float2(sc[i][r][2 * b], sc[i][r][2 * b + 1]), back), p = make_float2(ex2(d.x), ex2(d.y));
-            sum = add2(sum, p);
-            const float w0 = p.x * vs[2 * b], w1 = p.y * vs[2 * b + 1];
-            pa[i][b >> 1][(b & 1) * 2 + r] = pack_bf16(w0, w1);
-          }
-          l[i][r] += sum.x + sum.y;
-        }
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {                        // 16 keys: 16 b + t, + 4, + 8, + 12
-        uint2 v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int key = 16 * b + t + 4 * e;
-          v[e] = *reinterpret_cast<const uint2*>(s + 2048 + key * 64 + (((g >> 1) ^ (t & 2)) * 16) + (g & 1) * 8);
-        }
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {             // four columns: pairs of keys side by side, then one column of both a register
-          uint32_t w[2][2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const uint32_t x = half ? v[2 * e].y : v[2 * e].x, y = half ? v[2 * e + 1].y : v[2 * e + 1].x;
-            w[e][0] = __byte_perm(x, y, 0x5410);           // columns 0 and 1 of both, then 2 and 3
-            w[e][1] = __byte_perm(x, y, 0x7632);
-          }
-#pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            const uint32_t b0 = int8_to_bf16x2(w[0][d >> 1] >> (d & 1) * 8), b1 = int8_to_bf16x2(w[1][d >> 1] >> (d & 1) * 8);
-#pragma unroll
-            for (int i = 0; i < T; ++i) mma_bf16(o[i][4 * half + d], pa[i][b][0], pa[i][b][1], pa[i][b][2], pa[i][b][3], b0, b1);
-          }
-        }
       }
     }
+  };
+  if constexpr (PACK) {                                  // (loops of their own: with the choice inside one, a tenth slower)
+    if (wide) stream(std::false_type{});
+    else stream(std::true_type{});
+  } else {
+    stream(std::false_type{});
   }
   asm volatile("cp.async.wait_group 0;" ::: "memory");
   __syncwarp();
@@ -472,10 +517,6 @@ constexpr size_t kPlanesMost = (size_t)2 << 30;          // beyond which the few
 
 // 2^(x - 133) as a pair of bf16; NaN for 255.
 __device__ __forceinline__ uint32_t q8_step_bf16x2(uint32_t x) { return (x == 255u ? 0x7FFFu : (max(x, 6u) - 6u) << 7) * 0x00010001u; }
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
-  const __nv_bfloat162 d = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
-  return *reinterpret_cast<const uint32_t*>(&d);
-}
 
 // Where the live rows of each 64 of a sequence go among its live rows, and how many there are: they lie without gaps in the planes, so
 // the attention's loop knows no mask.  One CTA a sequence.
@@ -1114,7 +1155,7 @@ static inline int attn_q8_launch(AttnQ8Args P, void* scratch, cudaStream_t st, i
       *launches += 2;
     } else {
       const auto launch = [&](auto kernel, std::atomic<uint64_t>& smem_set) {
-        const int smem = few_smem_bytes(A.tile, A.warps);
+        const int smem = few_smem_bytes(A.warps);
         const cudaError_t set = allow_smem(kernel, smem, smem_set);
         return set != cudaSuccess ? set : launch_dependent(kernel, dim3((unsigned)ctas), A.warps * 32, 1, smem, st, true, P);
       };
