@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, few_warps(ROWS) / kFewWarps) k
 
   float m[T][R], l[T][R], o[T][8][4];                    // O: with at most 8 rows two columns a register pair, [0] and [1]
   int c1[PACK ? 8 : 1][4], c2[PACK ? 8 : 1][4], since = 0;   // what the int8 MMAs have summed up since O was last brought up to date, in how many tiles
-  float mv = -INFINITY;                                  // log2 of the reference weight
+  float mv = -INFINITY;                                  // log2 of the reference weight times step, over 2^m (the scores themselves may be far from zero)
 #pragma unroll
   for (int d = 0; d < (PACK ? 8 : 1); ++d)
 #pragma unroll
@@ -250,28 +250,28 @@ __global__ void __launch_bounds__(kFewWarps * 32, few_warps(ROWS) / kFewWarps) k
     for (int d = 0; d < 8; ++d) o[i][d][0] = o[i][d][1] = o[i][d][2] = o[i][d][3] = 0.0f;
   }
   auto stream = [&](auto by_bytes) {                     // the loop over this warp's tiles
-    constexpr bool kBytes = decltype(by_bytes)::value;     // Q by its bytes
+    constexpr bool kBytes = decltype(by_bytes)::value;   // Q by its bytes
     int stage = 0;
 #pragma unroll 1
     for (int tile = first; tile < tiles; tile += stride) {
       asm volatile("cp.async.wait_group %0;" ::"n"(kFewStages - 2) : "memory");
-      __syncwarp();                                        // this tile has arrived, and all lanes are done with the one before
+      __syncwarp();                                      // this tile has arrived, and all lanes are done with the one before
       request(tile + (kFewStages - 1) * stride, stage == 0 ? kFewStages - 1 : stage - 1);
       const unsigned char* s = stages + stage * kFewStage;
       stage = stage + 1 == kFewStages ? 0 : stage + 1;
 
-      {                                                    // a lane a row: what its scores and its weight are multiplied with
+      {                                                  // a lane a row: what its scores and its weight are multiplied with
         const bool in = tile * kFewKeys + lane < len && (P.live == nullptr || s[kFewX + 64 + lane] != 0);
         // (255: infinity, which a block of zeros makes NaN)
         const uint32_t vx = s[kFewX + 32 + lane];
         const float ks = __int_as_float((int)s[kFewX + lane] << 23);
-        if constexpr (PACK)                                // (the exponent of the value's step; a value that is not finite takes its score with it)
+        if constexpr (PACK)                              // (the exponent of the value's step; a value that is not finite takes its score with it)
           table[lane] = in ? make_float4(ks, vx == 255u ? __int_as_float(0x7FC00000) : 0.0f, (float)((int)vx - 133), 0.0f) : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
         else
           table[lane] = in ? make_float4(ks, 0.0f, q8_step(vx), 0.0f) : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
       }
       __syncwarp();
-      float sc[T][R][8], vs[8];                            // scores of keys 8 b + t (even entries) and 8 b + t + 4
+      float sc[T][R][8], vs[8];                          // scores of keys 8 b + t (even entries) and 8 b + t + 4
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         const uint4 kw = *reinterpret_cast<const uint4*>(s + (8 * b + g) * 64 + t * 16);
@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, few_warps(ROWS) / kFewWarps) k
 #pragma unroll
           for (int i = 0; i < T; ++i) c[i][0] = c[i][1] = c[i][2] = c[i][3] = 0.0f;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {                    // four bytes of a key: columns 0 and 2, 1 and 3
+          for (int j = 0; j < 4; ++j) {                  // four bytes of a key: columns 0 and 2, 1 and 3
             const uint32_t four = j == 0 ? kw.x : (j == 1 ? kw.y : (j == 2 ? kw.z : kw.w));
             const uint32_t b0 = int8_to_bf16x2(four), b1 = int8_to_bf16x2(four >> 8);
 #pragma unroll
@@ -329,17 +329,23 @@ __global__ void __launch_bounds__(kFewWarps * 32, few_warps(ROWS) / kFewWarps) k
           top[i][r] = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 2));
           grown |= top[i][r] > m[i][r] + kRescaleThreshold;
         }
-      float topv = -INFINITY;
-      if constexpr (PACK) {
+      auto top_weight = [&](float x) {                   // of the tile, over 2^x
+        const float ref = x == -INFINITY ? 0.0f : x;
+        float y = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) topv = fmaxf(topv, sc[0][0][e] + vs[e]);
-        topv = fmaxf(topv, __shfl_xor_sync(0xFFFFFFFFu, topv, 1));
-        topv = fmaxf(topv, __shfl_xor_sync(0xFFFFFFFFu, topv, 2));
+        for (int e = 0; e < 8; ++e) y = fmaxf(y, sc[0][0][e] - ref + vs[e]);
+        y = fmaxf(y, __shfl_xor_sync(0xFFFFFFFFu, y, 1));
+        return fmaxf(y, __shfl_xor_sync(0xFFFFFFFFu, y, 2));
+      };
+      if constexpr (PACK) {
+        const float topv = top_weight(m[0][0]);
         grown |= topv > mv + kRoom || since >= kSumsMost;
       }
       if (__any_sync(0xFFFFFFFFu, grown)) {
         if constexpr (PACK) {
-          const float mn = fmaxf(mv, topv);
+          const float to = fmaxf(m[0][0], top[0][0]);
+          if (m[0][0] != to) mv += m[0][0] - to;         // (both are -inf before the first live row)
+          const float mn = fmaxf(mv, top_weight(to));
           if (since > 0) take_sums(mv == mn ? 1.0f : ex2(mv - mn));
           mv = mn;
         }
@@ -360,13 +366,13 @@ __global__ void __launch_bounds__(kFewWarps * 32, few_warps(ROWS) / kFewWarps) k
           }
       }
       if constexpr (PACK) {
-        const float ref = m[0][0] == -INFINITY ? 0.0f : m[0][0], refv = mv == -INFINITY ? 0.0f : mv - kUnits;
-        const float2 back = make_float2(-ref, -ref), backv = make_float2(-refv, -refv);
+        const float ref = m[0][0] == -INFINITY ? 0.0f : m[0][0], up = kUnits - (mv == -INFINITY ? 0.0f : mv);
+        const float2 back = make_float2(-ref, -ref), up2 = make_float2(up, up);
         float2 sum = make_float2(0.0f, 0.0f);
         uint32_t w[8];
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-          const float2 x = make_float2(sc[0][0][2 * b], sc[0][0][2 * b + 1]), d = add2(x, back), y = add2(add2(x, make_float2(vs[2 * b], vs[2 * b + 1])), backv);
+          const float2 d = add2(make_float2(sc[0][0][2 * b], sc[0][0][2 * b + 1]), back), y = add2(add2(d, make_float2(vs[2 * b], vs[2 * b + 1])), up2);
           sum = add2(sum, make_float2(ex2(d.x), ex2(d.y)));
           w[2 * b] = __float2uint_rn(ex2(y.x));
           w[2 * b + 1] = __float2uint_rn(ex2(y.y));
@@ -382,11 +388,11 @@ __global__ void __launch_bounds__(kFewWarps * 32, few_warps(ROWS) / kFewWarps) k
           a2[2 * h] = x[1];
           a2[2 * h + 1] = x[0];
         }
-        uint2 v[8];                                        // rows t, t + 4, ...: the order of the weights
+        uint2 v[8];                                      // rows t, t + 4, ...: the order of the weights
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = *reinterpret_cast<const uint2*>(s + 2048 + (t + 4 * e) * 64 + (((g >> 1) ^ (t & 2)) * 16) + (g & 1) * 8);
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {             // four columns
+        for (int half = 0; half < 2; ++half) {           // four columns
           uint32_t b0[4], b1[4];
           transpose4(half ? v[0].y : v[0].x, half ? v[1].y : v[1].x, half ? v[2].y : v[2].x, half ? v[3].y : v[3].x, b0);
           transpose4(half ? v[4].y : v[4].x, half ? v[5].y : v[5].x, half ? v[6].y : v[6].x, half ? v[7].y : v[7].x, b1);
@@ -396,7 +402,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, few_warps(ROWS) / kFewWarps) k
             mma_u8s8(c2[4 * half + d], a2, b0[d], b1[d]);
           }
         }
-        ++since;                                           // (the same in every lane)
+        ++since;                                         // (the same in every lane)
       } else {
         uint32_t pa[T][2][4];                                // P of 16 keys as an operand
 #pragma unroll
@@ -454,7 +460,12 @@ __global__ void __launch_bounds__(kFewWarps * 32, few_warps(ROWS) / kFewWarps) k
 
   // ---- a warp's result into its stages: O [ROWS][64], the maxima, the sums
   float* mine = reinterpret_cast<float*>(stages);
-  if constexpr (PACK) take_sums(mv == -INFINITY ? 0.0f : ex2(mv - (m[0][0] == -INFINITY ? mv : m[0][0])) * 3.725290298461914e-09f);   // (2^-28)
+  if constexpr (PACK) {                                  // (2^(mv - 28) by halves: a value's step may be 2^-126, and with the units' 2^-28 their product is no fp32 number)
+    const float half = mv == -INFINITY ? 0.0f : ex2(0.5f * mv);
+    take_sums(half * 3.725290298461914e-09f);
+#pragma unroll
+    for (int d = 0; d < 8; ++d) o[0][d][0] *= half, o[0][d][1] *= half;
+  }
 #pragma unroll
   for (int i = 0; i < T; ++i)
 #pragma unroll

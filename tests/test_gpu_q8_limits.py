@@ -1,4 +1,4 @@
-"""Attention over an 8-bit cache where its arithmetic has least room: outliers in a query.
+"""Attention over an 8-bit cache where its arithmetic has least room: outliers in a query, tiny and far-apart values, scores far from zero.
 By 8, 16 and 32 rows of the streaming kernel and by planes."""
 import pytest
 import torch
@@ -59,3 +59,47 @@ def test_one_large_column_of_a_query(M, heads, kv, n, up):
     cache = B.new_cache_q8(1, n, kv)
     B.k_store_q8(cache, k, rnd(1, n, kv * 64))
     _check(q.bfloat16(), cache)
+
+
+@pytest.mark.parametrize("M,heads,kv,n", PATHS[:2])
+@pytest.mark.parametrize("kind", ["level", "ranging", "hidden"])
+@pytest.mark.parametrize("up", [-118, -60, 100])
+def test_values_of_any_size(M, heads, kv, n, kind, up):
+    """Values about 2^up: all alike; down to 2^-7 of that in turn; or behind one row of zeros that weighs 2^9 times any other's."""
+    g = _g(M + n + up)
+    rnd = lambda *s: torch.randn(s, generator=g, device="cuda")
+    v = rnd(1, n, kv * 64).double()
+    k = rnd(1, n, kv * 64) * 0.25
+    q = torch.ones((1, M, heads * 64), device="cuda") + 0.25 * rnd(1, M, heads * 64)
+    if kind == "ranging":
+        v *= torch.exp2(-(torch.arange(n, device="cuda") % 8).double())[None, :, None]
+    if kind == "hidden":
+        k[0, n // 3] = 9 * 0.6931 / 8
+        v[0, n // 3] = 0
+    cache = B.new_cache_q8(1, n, kv)
+    B.k_store_q8(cache, k, (v * 2.0 ** up).float())
+    _check(q.bfloat16(), cache)
+
+
+@pytest.mark.parametrize("M,heads,kv,n", PATHS)
+@pytest.mark.parametrize("size", [1e3, 1e6, 1e9, -1e3, -1e9])
+def test_scores_far_from_zero(M, heads, kv, n, size):
+    """All keys alike, so that every score is the same large number: the result is the mean of the values."""
+    if abs(size) > 2.0 ** 30 and M > 1000:
+        return                                           # (more than what is promised; the streaming kernel does it)
+    g = _g(M + n)
+    cache = B.new_cache_q8(3, n, kv)
+    k = torch.zeros((3, n, kv, 64), device="cuda")
+    k[..., 0] = 2.0 ** 20 if abs(size) < 2.0 ** 60 else 2.0 ** 60
+    v = torch.randn((3, n, kv * 64), generator=g, device="cuda")
+    v *= torch.exp2(-(torch.arange(n, device="cuda") % 8).float())[None, :, None]
+    B.k_store_q8(cache, k.view(3, n, -1), v)
+    q = torch.zeros((3, M, heads, 64), device="cuda")
+    q[..., 0] = size * 8 / float(k.max())
+    lens = torch.tensor([n, 37, n // 2], dtype=torch.int32, device="cuda")
+    out = B.k_attention_q8(q.view(3, M, -1).bfloat16(), cache, lens=lens).double().view(3, M, heads, 64)
+    back = B.k_load_q8(cache, n, dtype=torch.float32)[1].double().view(3, n, kv, 64)
+    for s in range(3):
+        x = back[s, :int(lens[s])].repeat_interleave(heads // kv, 1)
+        tol = 2.0 ** -8 * x.mean(0).abs() + (1e-5 + (0 if M * heads // kv <= 8 else 2.0 ** -8)) * x.abs().mean(0) + 2.0 ** -28 * n * x.abs().amax(0)
+        assert bool(((out[s] - x.mean(0)).abs() <= tol).all())
