@@ -242,6 +242,10 @@ __global__ void __launch_bounds__(kFewWarps * 32, few_warps(ROWS) / kFewWarps) k
   };
   constexpr float kUnits = 28.0f, kRoom = 3.0f;          // a reference weight is 2^28 units; another is at most 2^3 of it
   constexpr int kSumsMost = 2000;                        // tiles: 64000 x 255 x 127 is below 2^31
+  // With more rows O is in units of 2^(xv - 133), so that a weight times a value's step is a number bf16 holds whatever the values' size: xv is
+  // the largest exponent seen, or up to 2^4 below it.
+  int xv = 7;
+  constexpr int kRoomX = 4;
 #pragma unroll
   for (int i = 0; i < T; ++i) {
 #pragma unroll
@@ -267,8 +271,22 @@ __global__ void __launch_bounds__(kFewWarps * 32, few_warps(ROWS) / kFewWarps) k
         const float ks = __int_as_float((int)s[kFewX + lane] << 23);
         if constexpr (PACK)                              // (the exponent of the value's step; a value that is not finite takes its score with it)
           table[lane] = in ? make_float4(ks, vx == 255u ? __int_as_float(0x7FC00000) : 0.0f, (float)((int)vx - 133), 0.0f) : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
-        else
-          table[lane] = in ? make_float4(ks, 0.0f, q8_step(vx), 0.0f) : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
+        else {
+          const int most = in && vx != 255u ? (int)vx : 0;
+          if (__any_sync(0xFFFFFFFFu, most > xv + kRoomX)) {
+            const int to = __reduce_max_sync(0xFFFFFFFFu, most);
+            const float down = to - xv > 126 ? 0.0f : __int_as_float((127 - (to - xv)) << 23);
+            xv = to;
+#pragma unroll
+            for (int i = 0; i < T; ++i)
+#pragma unroll
+              for (int d = 0; d < 8; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[i][d][e] *= down;
+          }
+          const float vs = vx == 255u ? __int_as_float(0x7FC00000) : __int_as_float(max((int)vx - xv + 127, 0) << 23);
+          table[lane] = in ? make_float4(ks, 0.0f, vs, 0.0f) : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
+        }
       }
       __syncwarp();
       float sc[T][R][8], vs[8];                          // scores of keys 8 b + t (even entries) and 8 b + t + 4
@@ -465,6 +483,14 @@ __global__ void __launch_bounds__(kFewWarps * 32, few_warps(ROWS) / kFewWarps) k
     take_sums(half * 3.725290298461914e-09f);
 #pragma unroll
     for (int d = 0; d < 8; ++d) o[0][d][0] *= half, o[0][d][1] *= half;
+  } else {
+    const float units = __int_as_float((xv - 6) << 23);
+#pragma unroll
+    for (int i = 0; i < T; ++i)
+#pragma unroll
+      for (int d = 0; d < 8; ++d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[i][d][e] *= units;
   }
 #pragma unroll
   for (int i = 0; i < T; ++i)

@@ -61,7 +61,7 @@ def test_one_large_column_of_a_query(M, heads, kv, n, up):
     _check(q.bfloat16(), cache)
 
 
-@pytest.mark.parametrize("M,heads,kv,n", PATHS[:2])
+@pytest.mark.parametrize("M,heads,kv,n", PATHS)
 @pytest.mark.parametrize("kind", ["level", "ranging", "hidden"])
 @pytest.mark.parametrize("up", [-118, -60, 100])
 def test_values_of_any_size(M, heads, kv, n, kind, up):
