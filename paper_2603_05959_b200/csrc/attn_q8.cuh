@@ -21,7 +21,7 @@ struct AttnQ8Args {
 
 // What stands for a part without live rows: a maximum below every other's, so that it weighs nothing beside a part that has some, and
 // a sum that makes the result zero where no part has.
-constexpr float kDeadMax = -1e30f, kDeadSum = 1.0f;
+constexpr float kDeadMax = -3.4e38f, kDeadSum = 1.0f;
 
 __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"

@@ -82,7 +82,7 @@ def test_values_of_any_size(M, heads, kv, n, kind, up):
 
 
 @pytest.mark.parametrize("M,heads,kv,n", PATHS)
-@pytest.mark.parametrize("size", [1e3, 1e6, 1e9, -1e3, -1e9])
+@pytest.mark.parametrize("size", [1e3, 1e6, 1e9, -1e3, -1e9, -1e33])
 def test_scores_far_from_zero(M, heads, kv, n, size):
     """All keys alike, so that every score is the same large number: the result is the mean of the values."""
     if abs(size) > 2.0 ** 30 and M > 1000:
