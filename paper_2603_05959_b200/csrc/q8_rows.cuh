@@ -116,13 +116,39 @@ __global__ void __launch_bounds__(norm_cta(THREADS)) k_norm_q8(const NormQ8Args 
   }
   const auto add = [](float a, float b) { return a + b; };
   if (!PLAIN && P.kind != OVGGT_NORM_NONE) {
-    if (P.kind == OVGGT_NORM_LAYER) {
+    float eps = P.eps;
+    const auto sum = [&]() {
       float s = 0.0f;
 #pragma unroll
       for (int i = 0; i < U; ++i)
 #pragma unroll
         for (int e = 0; e < 8; ++e) s += y[i][e];
-      const float mean = row_reduce<THREADS>(s, sh, add) / (float)P.C;
+      return row_reduce<THREADS>(s, sh, add);
+    };
+    const auto squares = [&]() {
+      float s = 0.0f;
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s = fmaf(y[i][e], y[i][e], s);
+      return row_reduce<THREADS>(s, sh, add);
+    };
+    // A row whose sum or squares leave fp32's range is taken times a power of two, and eps with it.  (The norm does not change; a row's threads all
+    // have its sums, a warp's rows go through the shuffles together.)
+    const auto rescale = [&](float by) {
+      if (THREADS <= 32 ? __all_sync(0xFFFFFFFFu, by == 1.0f) != 0 : by == 1.0f) return false;
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[i][e] *= by;
+      eps = eps * by * by;
+      return true;
+    };
+    constexpr float kDown = 8.271806125530277e-25f, kUp = 1.2676506002282294e30f;        // 2^-80, 2^100
+    if (P.kind == OVGGT_NORM_LAYER) {
+      float s = sum();
+      if (rescale(fabsf(s) < INFINITY ? 1.0f : kDown)) s = sum();
+      const float mean = s / (float)P.C;
 #pragma unroll
       for (int i = 0; i < U; ++i)
         if (tid + i * THREADS < units) {
@@ -130,12 +156,10 @@ __global__ void __launch_bounds__(norm_cta(THREADS)) k_norm_q8(const NormQ8Args 
           for (int e = 0; e < 8; ++e) y[i][e] -= mean;
         }
     }
-    float s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < U; ++i)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s = fmaf(y[i][e], y[i][e], s);
-    const float rstd = 1.0f / sqrtf(row_reduce<THREADS>(s, sh, add) / (float)P.C + P.eps);
+    float s = squares();
+    // (below 2^-90 and above 2^-80: what s lacks does not show beside eps)
+    if (rescale(!(s < INFINITY) ? kDown : (s < 8.077935669463161e-28f && eps < 8.271806125530277e-25f ? kUp : 1.0f))) s = squares();
+    const float rstd = 1.0f / sqrtf(s / (float)P.C + eps);
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const int u = tid + i * THREADS;
