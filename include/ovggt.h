@@ -376,7 +376,7 @@ enum { OVGGT_NORM_NONE = 0, OVGGT_NORM_RMS = 1, OVGGT_NORM_LAYER = 2 };
  * to even.  x, residual, sum [rows, C], weight, bias [C] in dtype; q [rows, C] int8; scale [rows] fp32.  residual, weight, bias and sum may
  * be NULL (weight and bias are NULL for OVGGT_NORM_NONE); sum takes h and needs a residual; it may be x or residual.  Statistics are
  * fp32, of rows of any size.  A row whose y is not finite gets a scale that is not a number and zeros in q; one whose |y| stays below 2^-119 a
- * scale of 0 and zeros.  C a multiple of 16, up to 16384 (OVGGT_ERR_UNSUPPORTED). */
+ * scale of 0 and zeros.  C a multiple of 16, up to 16384; up to 2^31 - 256 rows (OVGGT_ERR_UNSUPPORTED). */
 int ovggt_k_norm_q8(const void* x, const void* residual, const void* weight, const void* bias, int32_t rows, int32_t C,
                     int32_t dtype, int32_t kind, float eps, void* sum, int8_t* q, float* scale, void* stream);
 

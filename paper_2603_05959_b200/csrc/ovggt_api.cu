@@ -1602,7 +1602,7 @@ extern "C" int ovggt_k_norm_q8(const void* x, const void* residual, const void* 
   if (!x || !q || !scale || rows < 0 || C < 1 || (dtype != kF32 && dtype != kBF16) || kind < OVGGT_NORM_NONE || kind > OVGGT_NORM_LAYER ||
       (sum && !residual) || (kind == OVGGT_NORM_NONE && (weight || bias)) || !(eps >= 0.0f))
     return OVGGT_ERR_INVALID_ARG;
-  if (C % 16 != 0 || C > kNormMaxC) return OVGGT_ERR_UNSUPPORTED;
+  if (C % 16 != 0 || C > kNormMaxC || rows > 0x7FFFFF00) return OVGGT_ERR_UNSUPPORTED;   // (the grid is counted in 32 bits)
   if (!aligned16(x) || !aligned16(residual) || !aligned16(weight) || !aligned16(bias) || !aligned16(sum) || !aligned16(q) || !aligned(scale, 4))
     return OVGGT_ERR_MISALIGNED;
   NormQ8Args P = {};

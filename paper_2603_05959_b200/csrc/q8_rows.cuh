@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(norm_cta(THREADS)) k_norm_q8(const NormQ8Args 
     for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(y[i][e]) & 0x7FFFFFFFu);
   most = __float_as_uint(row_reduce<THREADS>(__uint_as_float(most), sh, [](float a, float b) { return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b))); }));
   // A row with a value that is not finite gets a scale that is not a number, and products of it are none; a row of
-  // nothing but (almost) zeros a scale of 0: below 2^-119, 127 / maximum has no fp32 value.
+  // nothing but (almost) zeros a scale of 0: down to 2^-119 maximum / 127 is a normal number, and 127 / maximum one of fp32's.
   const float amax = __uint_as_float(most);
   const bool finite = most < 0x7F800000u, some = finite && amax >= 1.504632769052528e-36f;
   const float inv = some ? 127.0f / amax : 0.0f;

@@ -1,0 +1,8 @@
+"""CPU checks of the 8-bit entry points at the ends of their ranges: refused before a GPU is touched."""
+from test_abi_q8 import ATTEND, BAD, LINEAR, MISALIGNED, NORM, P, UNSUPPORTED, _call, lib  # noqa: F401  (the fixture builds the library)
+
+
+def test_rows_that_a_grid_cannot_count(lib):  # noqa: F811
+    """Sixteen rows of up to 256 columns share a CTA: the count of CTAs, rounded up, would pass 32 bits."""
+    for rows in (0x7FFFFFFF, 0x7FFFFFF1, 0x7FFFFF01):
+        assert _call(lib.ovggt_k_norm_q8, list(NORM), NORM, rows=rows, C=16) == UNSUPPORTED
