@@ -1628,7 +1628,8 @@ extern "C" int ovggt_k_linear_q8(const int8_t* A, const float* a_scale, const in
       (n_outs > 0 && !outs) || (residual != nullptr) != (sum != nullptr) || (n_outs == 0 && !sum))
     return OVGGT_ERR_INVALID_ARG;
   if (K % 16 != 0 || K > kQ8MaxK || N % 8 != 0 || M > 0x7FFFFF00 || N > 0x7FFFFF00 || (n_outs > 1 && (N % n_outs != 0 || (N / n_outs) % 8 != 0))) return OVGGT_ERR_UNSUPPORTED;
-  if (!aligned16(A) || !aligned16(W) || !aligned(a_scale, 4) || !aligned16(w_scale) || !aligned16(residual) || !aligned16(sum))
+  if (!aligned16(A) || !aligned16(W) || !aligned(a_scale, 4) || !aligned16(w_scale) || !aligned16(residual) || !aligned16(sum) ||
+      !aligned(device_status, 4))
     return OVGGT_ERR_MISALIGNED;
   GemmQ8Args P = {};
   P.o.M = M; P.o.N = N; P.o.K = K;

@@ -6,3 +6,8 @@ def test_rows_that_a_grid_cannot_count(lib):  # noqa: F811
     """Sixteen rows of up to 256 columns share a CTA: the count of CTAs, rounded up, would pass 32 bits."""
     for rows in (0x7FFFFFFF, 0x7FFFFFF1, 0x7FFFFF01):
         assert _call(lib.ovggt_k_norm_q8, list(NORM), NORM, rows=rows, C=16) == UNSUPPORTED
+
+
+def test_a_status_word_that_cannot_be_written(lib):  # noqa: F811
+    for by in (1, 2, 3):
+        assert _call(lib.ovggt_k_linear_q8, list(LINEAR), LINEAR, status=P + by) == MISALIGNED
