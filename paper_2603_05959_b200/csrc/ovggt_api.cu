@@ -1705,10 +1705,11 @@ extern "C" int ovggt_k_attention_q8(const void* q, const int8_t* kq, const uint8
                                     int32_t M, int32_t n_heads, int32_t n_kv_heads, int32_t capacity, const int32_t* lens,
                                     const uint8_t* live, void* out, void* scratch, int32_t* device_status, void* stream) {
   if (n_seqs == 0 || M == 0) return OVGGT_OK;
-  if (!q || !kq || !kx || !vq || !vx || !out || !scratch || !device_status || n_seqs < 0 || M < 0 || n_heads < 1 || n_kv_heads < 1 || capacity < 1 ||
+  if (!q || !kq || !kx || !vq || !vx || !out || !device_status || n_seqs < 0 || M < 0 || n_heads < 1 || n_kv_heads < 1 || capacity < 1 ||
       n_heads % n_kv_heads != 0)
     return OVGGT_ERR_INVALID_ARG;
-  if (!attention_q8_fits(n_seqs, M, n_heads, capacity)) return OVGGT_ERR_UNSUPPORTED;
+  if (!attention_q8_fits(n_seqs, M, n_heads, capacity)) return OVGGT_ERR_UNSUPPORTED;   // (for which there is no scratch size either)
+  if (!scratch) return OVGGT_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(out) || !aligned16(scratch) || !aligned16(kq) || !aligned16(vq) || !aligned16(kx) || !aligned16(vx) || !aligned16(live) ||
       !aligned(lens, 4) || !aligned(device_status, 4))
     return OVGGT_ERR_MISALIGNED;
