@@ -607,10 +607,14 @@ def k_norm_q8(x: torch.Tensor, weight=None, bias=None, residual=None, kind=NORM_
 
 def k_linear_q8(a, a_scale, w, w_scale, outs=(), gelu=False, residual=None, sum_out=None, status=None, stream=None) -> None:
     """t = (a a_scale) [M, K] @ (w w_scale) [N, K] ^T (then GELU), int8 operands; its column blocks to outs; sum_out = residual + t.
-    Nothing is allocated."""
+    Nothing is allocated where a status word is given; without one the call waits for the product and raises if it failed."""
     (M, K), N, n = a.shape, w.shape[0], len(outs)
     assert w.shape[1] == K and a.dtype is _I8 and w.dtype is _I8
     assert a_scale.shape == (M,) and w_scale.shape == (N,) and a_scale.dtype is _F32 and w_scale.dtype is _F32
+    own = status is None
+    if own:
+        with torch.cuda.stream(stream):
+            status = torch.zeros(16, dtype=_I32, device=a.device)
     assert n <= 3 and status.numel() * status.element_size() >= 4
     d = torch._C._cuda_getDevice()
     at = (C.c_void_p * 3)()
@@ -623,6 +627,9 @@ def k_linear_q8(a, a_scale, w, w_scale, outs=(), gelu=False, residual=None, sum_
                                    _at(sum_out, d), _at(status, d), _stream_ptr(stream))
     if code:
         _check(code, "ovggt_k_linear_q8")
+    if own:
+        with torch.cuda.stream(stream):
+            _check(int(status[0].item()), "ovggt_k_linear_q8 (device status)")
 
 
 def new_cache_q8(n_seqs: int, capacity: int, n_heads: int, device=None):
