@@ -17,12 +17,12 @@ def _g(seed):
     return g
 
 
-def _check(q, cache, lens=None):
+def _check(q, cache, lens=None, live=None):
     """Against fp64 by what the cache stands for.  What may be off: a score by the fp32 sums of 64 exact products in four steps of 16, each of 17
     terms cut to 2^-22 of the largest, 2^-17 of the sum of magnitudes in all; a weight by 1e-5 (exponentials, fp32 sums), from 9 rows of a
     key head on also by its rounding to bf16, 2^-8, and up to 8 by half of 2^-28 of the largest weight times step, 127 of which a value has at most;
     the result by its own rounding."""
-    out = B.k_attention_q8(q, cache, lens=lens)
+    out = B.k_attention_q8(q, cache, lens=lens, live=live)
     seqs, M, _ = q.shape
     capacity, kv = cache[0].shape[1], cache[0].shape[2] // 64
     H = q.shape[2] // 64
@@ -30,9 +30,15 @@ def _check(q, cache, lens=None):
     k, v = (x.double().view(seqs, capacity, kv, 64) for x in B.k_load_q8(cache, capacity, dtype=torch.float32))
     worst = 0.0
     for s in range(seqs):
-        n = capacity if lens is None else int(lens[s])
+        keep = torch.arange(capacity, device="cuda") < (capacity if lens is None else int(lens[s]))
+        if live is not None:
+            keep &= live[s] != 0
+        n = int(keep.sum())
+        if n == 0:
+            assert not bool(out[s].any())
+            continue
         for h in range(H):
-            qh, kh, vh = q[s, :, h * 64:h * 64 + 64].double(), k[s, :n, h * kv // H], v[s, :n, h * kv // H]
+            qh, kh, vh = q[s, :, h * 64:h * 64 + 64].double(), k[s, :, h * kv // H][keep], v[s, :, h * kv // H][keep]
             p = torch.softmax(qh @ kh.T / 8, -1)
             ref, spread = p @ vh, p @ vh.abs()
             ds = (qh.abs() @ kh.abs().T).amax(-1, keepdim=True) / 8 * 2.0 ** -17
