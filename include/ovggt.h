@@ -373,7 +373,7 @@ int ovggt_k_linear_bf16(const void* A, const void* B, int32_t M, int32_t N, int3
 enum { OVGGT_NORM_NONE = 0, OVGGT_NORM_RMS = 1, OVGGT_NORM_LAYER = 2 };
 
 /* h = x + residual (rounded to dtype), or x; y = norm(h) * weight + bias; scale[row] = max |y| / 127, q = round(y / scale), ties
- * to even.  x, residual, sum [rows, C], weight, bias [C] in dtype; q [rows, C] int8; scale [rows] fp32.  residual, weight, bias and sum may
+ * to even (the quotient is y times 127 / max |y| in fp32).  x, residual, sum [rows, C], weight, bias [C] in dtype; q [rows, C] int8; scale [rows] fp32.  residual, weight, bias and sum may
  * be NULL (weight and bias are NULL for OVGGT_NORM_NONE); sum takes h and needs a residual; it may be x or residual.  Statistics are
  * fp32, of rows of any size.  A row whose y is not finite gets a scale that is not a number and zeros in q; one whose |y| stays below 2^-119 a
  * scale of 0 and zeros.  C a multiple of 16, up to 16384; up to 2^31 - 256 rows (OVGGT_ERR_UNSUPPORTED). */
@@ -404,8 +404,10 @@ int ovggt_k_load_q8(const int8_t* kq, const uint8_t* kx, const int8_t* vq, const
 /* out [n_seqs, M, n_heads * 64] = softmax(Q K^T / sqrt(64)) V over the rows of an 8-bit cache, bf16 queries and output: row j of sequence s
  * takes part if j < lens[s] (device [n_seqs], NULL = capacity; taken as 0 below 0 and as capacity above it) and live[s, j] != 0 (device
  * [n_seqs, capacity] uint8, NULL = all).  Where no row does, out is 0.  Query head h reads key head h / (n_heads / n_kv_heads); n_heads
- * a multiple of n_kv_heads.  Rows that do not take part may hold anything.  scratch: device, >= ovggt_k_attention_q8_scratch_bytes
- * (0 if the sizes are invalid); it need not hold anything, and calls that may overlap need one each.  device_status: device int, as for
+ * a multiple of n_kv_heads.  Rows that do not take part may hold anything.  Queries and cached values count with every bit; scores, exponentials and
+ * sums are fp32.  With up to 8 rows (tokens times query heads of a key head) a weight times its value's step is rounded to 2^-28 of the largest,
+ * with more a weight to bf16; with many, for which the cache is widened into scratch, exponentials are right to 1e-4.  Scores up to 2^30 and values
+ * up to 2^100 in size.  scratch: device, >= ovggt_k_attention_q8_scratch_bytes (0 if the sizes are invalid); it need not hold anything, and calls that may overlap need one each.  device_status: device int, as for
  * ovggt_k_attention. */
 size_t ovggt_k_attention_q8_scratch_bytes(int32_t n_seqs, int32_t M, int32_t n_heads, int32_t n_kv_heads, int32_t capacity);
 int ovggt_k_attention_q8(const void* q, const int8_t* kq, const uint8_t* kx, const int8_t* vq, const uint8_t* vx, int32_t n_seqs,

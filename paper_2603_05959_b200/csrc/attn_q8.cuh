@@ -64,22 +64,22 @@ __device__ __forceinline__ uint32_t int8_to_bf16x2(uint32_t x) { return sub_bf16
 
 // ---------------------------------------------------------------- few rows: the cache streams through, once per 8, 16 or 32 rows
 //
-// What bounds it: the cache's bytes (the copies alone take 10 of 18 us of one row over 32768), and beside them the arithmetic on them, chains of
+// What bounds it: the cache's bytes (the copies alone take 10 of 20 us of one row over 32768), and beside them the arithmetic on them, chains of
 // copy, MMA, exponentials and MMA that a dozen warps an SM do not cover.  A warp takes tiles of 32 cached rows by itself, with three of them on their way in its own stages
 // (no barrier in the loop); the warps' results are joined through shared memory, those of the CTAs that share a sequence and head (parts) by
 // the bf16 attention's merge kernel.
 //   scores  from queries that keep every bit.  With at most 8 rows by int8 MMAs on the cached bytes as they are: a row of Q is taken as whole
 //           numbers of 31 bits in units of 2^-29 of its largest power of two, four int8 operands in the halves of two; where that would not
 //           be exact (a row with elements below 2^-22 of its largest), and with more rows, by bf16 MMAs on Q itself and the cached bytes
-//           made bf16.  (One row over 32768, 16 heads: 19.5 us, by bf16 MMAs 22.0; two operands' 15 bits took 18.4 and lost a row's small elements.)
+//           made bf16.  (One row over 32768, 16 heads: 20.0 us, by bf16 MMAs 22.0; two operands' 15 bits took 18.4 and lost a row's small elements.)
 //   P V     with at most 8 rows by int8 MMAs too: a weight p 2^(x - 133) as a whole number of 31 bits, 2^-28 of a reference that follows the largest
 //           weight, four unsigned bytes in the halves of two operands; the cached bytes of four rows are only put side by side.  The int32 sums
 //           are exact and go into fp32 when the reference moves.  With more rows, where that many sums do not fit the registers, by bf16 MMAs: the
 //           cached bytes are exact in bf16, a weight is rounded to it (2^-8).
 // Which cached row or column an operand's row or column stands for is free, so each lane takes 16 bytes of a K row and 8
 // bytes of a V row at once.
-// An SM holds as many warps as their registers leave without spilling (four tokens over up to 16384 rows by 16 warps 28 us, by 12 25; 16 rows
-// over 2048 8.6 and 7.9; 32 rows over 8192 by 12 warps 16.5, by 8 13.7), in one CTA or in two or three smaller ones (see attn_q8_plan).
+// An SM holds as many warps as their registers leave without spilling (with queries of 15 bits four tokens over up to 16384 rows by 16 warps 28 us, by
+// 12 25, now 29; 16 rows over 2048 8.6 and 7.9, now 8.0; 32 rows over 8192 by 12 warps 16.5, by 8 13.7, now 14.3), in one CTA or in two or three smaller ones (see attn_q8_plan).
 __host__ __device__ constexpr int few_warps(int rows) { return rows == 32 ? 8 : 12; }
 constexpr int kFewStages = 3, kFewKeys = 32;
 constexpr int kFewX = 2 * kFewKeys * 64;                 // of a stage: K, V, then the exponents of K and V and the mask, 32 bytes each
@@ -546,7 +546,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, few_warps(ROWS) / kFewWarps) k
 // ---------------------------------------------------------------- many rows: tcgen05 over bf16 planes
 //
 // From some tiles of queries on (see attn_q8_by_planes), widening the cache once, into bf16 planes in scratch memory, costs less than each tile's
-// doing it: a plane takes some 3 instructions an element and 5 bytes of traffic, most of it in L2 (17758 rows of 16 heads: 22 us beside 128 of
+// doing it: a plane takes some 3 instructions an element and 5 bytes of traffic, most of it in L2 (17758 rows of 16 heads: 22 us, 26 from memory, beside 128 of
 // attention and merge for 11 tiles of queries; widened on the way into shared memory, once for two tiles, the same attention took 250 us: the
 // widening warps share the issue slots with the softmax).  The planes are what the cache stands for: q 2^(x - 133) is exact in bf16.
 constexpr size_t kPlanesAtOnce = (size_t)128 << 20;      // bytes of planes up to which sequences are taken together: what stays in L2
@@ -1096,8 +1096,8 @@ k_attn_q8_many(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
 
 // Whether a call goes by way of planes, from its time in picoseconds: streaming the cache costs 5 us and 45 ps a cached row, head and 32
 // rows of queries; the planes 11 us, 118 ps a cached row and head, and 25 ps more for each 128 rows of queries after the first.  Fitted to 96 to
-// 512 rows over 512 to 32768 of 16 heads: 96 x 8192 23.6 us against 26.7, 128 x 8192 30.4 against 27.1, 256 x 2048 17.0 against 19.3, 256 x 8192
-// 51.9 against 30.4.
+// 512 rows over 512 to 32768 of 16 heads, with queries of 15 bits where they stream.  Now 64 x 8192 21.3 us against 26.5, 96 x 8192 26.8 against 26.7, 128 x 8192
+// 34.0 against 27.1, 256 x 2048 19.2 against 20.0, 256 x 8192 55.7 against 30.9, 512 x 2048 32.2 against 21.9.
 inline bool attn_q8_by_planes(long long cached, long long rows) {      // cached rows times heads, over all sequences
   const double x = (double)cached;
   return 5e6 + 45.0 * x * (double)((rows + 31) / 32) > 11e6 + x * (118.0 + 25.0 * (double)((rows - 1) / kBM));
@@ -1132,7 +1132,8 @@ inline AttnQ8Plan attn_q8_plan(int seqs, int M, int H, int HK, int cap) {
     A.q_tiles = (int)((rows + A.tile - 1) / A.tile);
     // Warps a CTA and parts, by a model of the time in 10 ns: waves of CTAs over 148 SMs, each as long as a warp's tiles of 32 cached rows (a last
     // one shorter, which has the SMs to itself) and its set-up and end, which smaller CTAs hide under one another's work, and a merge.  Fitted to 16 to 1024 sequences times heads over 256 to 32768 rows: 16 x
-    // 32768 by 12 warps 18 us, by 6 19, by 4 24; 80 x 8192 24, 19 and 17; 256 x 2048 20, 15.5 and 20; 1024 x 2048 66, 51 and 47.
+    // 32768 by 12 warps 20 us, by 6 21, by 4 27; 80 x 8192 21, 21 and 19; 256 x 2048 21, 17.6 and 20; 1024 x 2048 71, 59 and 54.  (480 x 8192
+    // takes 99 us as chosen, 84 by 4: the constants are those of queries of 15 bits, whose tiles took a tenth less.)
     const long long jobs = (long long)seqs * HK * A.q_tiles, tiles = (cap + kFewKeys - 1) / kFewKeys;
     const int whole = few_warps(A.tile), step = A.tile == 8 ? 115 : (A.tile == 16 ? 168 : 157);
     long long best = -1;

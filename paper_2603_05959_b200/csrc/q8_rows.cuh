@@ -54,9 +54,9 @@ __device__ __forceinline__ float row_reduce(float x, float* sh, Op op) {
 
 // Four groups of eight elements a thread, whatever the row's width: 8 to 512 threads a row, several rows a CTA where they are less than
 // 128.  All loads, the weight's among them, are requested before the first reduction.  What bounds it is memory (10992 x 1024 bf16 with a
-// residual: 79 MB in 12.3 us, 6.4 TB/s), of a single row the trip to it: with one to four groups a thread, a warp up to 1024 columns and a CTA beyond, and weights
+// residual: 79 MB in 15.8 us, 5.0 TB/s; 12.9 where they still are in L2), of a single row the trip to it: with one to four groups a thread, a warp up to 1024 columns and a CTA beyond, and weights
 // read where they are needed, 60000 x 256 took 23.6 us instead of 18.1, 4000 x 8192 59 instead of 40 and one row of 1024 3.5 instead of 2.4.
-// PLAIN: neither a residual nor a norm, in instances with registers for no more (10992 x 4096: 25.1 us, without them 29.8).
+// PLAIN: neither a residual nor a norm, in instances with registers for no more (10992 x 4096: 25.2 us, without them 29.8).
 constexpr int kNormUnits = 4;
 __host__ __device__ constexpr int norm_cta(int threads) { return threads < 128 ? (threads == 64 ? 64 : 128) : threads; }
 template <int DT, int THREADS, bool PLAIN>
@@ -282,8 +282,8 @@ __device__ __forceinline__ float int8_at(uint32_t flipped) {   // (flipped: the 
 }
 
 // Bound by memory.  Whole lines both ways: four groups of 16 bytes of output a thread, a CTA's width apart; stores that leave L2 first, since what
-// is read back is as a rule larger than it.  17758 rows of 16 heads: bf16 18.1 us (6.0 TB/s), fp32 30.0; with ordinary stores 20.8 and 36.4, with
-// 16 elements a thread side by side 19.8 and 41.7, with eight groups a thread 21.3 and 31.0.
+// is read back is as a rule larger than it.  17758 rows of 16 heads: bf16 23 us (4.7 TB/s), fp32 37.8 (4.8).  With the cache in L2 17.6 and 30.4; so measured
+// with ordinary stores 20.8 and 36.4, with 16 elements a thread side by side 19.8 and 41.7, with eight groups a thread 21.3 and 31.0.
 constexpr int kLoadGroups = 4;
 template <int DT>
 __global__ void __launch_bounds__(256) k_load_q8(const LoadQ8Args P) {
