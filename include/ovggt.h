@@ -406,8 +406,8 @@ int ovggt_k_load_q8(const int8_t* kq, const uint8_t* kx, const int8_t* vq, const
  * [n_seqs, capacity] uint8, NULL = all).  Where no row does, out is 0.  Query head h reads key head h / (n_heads / n_kv_heads); n_heads
  * a multiple of n_kv_heads.  Rows that do not take part may hold anything.  Queries and cached values count with every bit; scores, exponentials and
  * sums are fp32.  With up to 8 rows (tokens times query heads of a key head) a weight times its value's step is rounded to 2^-28 of the largest,
- * with more a weight to bf16; with many, for which the cache is widened into scratch, exponentials are right to 1e-4.  Scores up to 2^30 and values
- * up to 2^100 in size.  scratch: device, >= ovggt_k_attention_q8_scratch_bytes (0 if the sizes are invalid); it need not hold anything, and calls that may overlap need one each.  device_status: device int, as for
+ * with more a weight to bf16; with many, for which the cache is widened into scratch, exponentials are right to 1e-4.  Scores up to 2^30, values up to
+ * 2^100 and products of a query's and a key's largest elements up to 2^120 in size.  scratch: device, >= ovggt_k_attention_q8_scratch_bytes (0 if the sizes are invalid); it need not hold anything, and calls that may overlap need one each.  device_status: device int, as for
  * ovggt_k_attention. */
 size_t ovggt_k_attention_q8_scratch_bytes(int32_t n_seqs, int32_t M, int32_t n_heads, int32_t n_kv_heads, int32_t capacity);
 int ovggt_k_attention_q8(const void* q, const int8_t* kq, const uint8_t* kx, const int8_t* vq, const uint8_t* vx, int32_t n_seqs,
